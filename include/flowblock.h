@@ -411,6 +411,55 @@ int fb_gate_commit(fb_ctx* ctx, const fb_pack* pk, const int32_t* slot_stats,
                    uint8_t* spawned, int32_t* step_counters, int32_t* status,
                    void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Decoding one token at a time over the same pages: a request whose window is a
+ * single token (an autoregressive model, or a verifier, beside the block
+ * decoder), and a single query that weighs the keys of a frozen prefix.  The
+ * paper has no counterpart (its serial decoder works block by block); the page
+ * layout, the head grouping and the scales of 8-bit pages are those of the
+ * calls above.  Three calls make a step of a layer: fb_append_kv stores the new
+ * token, fb_token_attn attends to everything stored, fb_evict_kv cuts a cache
+ * that has outgrown its bound.
+ *
+ * C = 64 * max_pages_per_req is the capacity of a request.  Per request:
+ *   kv_len     [R_max] keys stored, the newest token's included.  0: none yet.
+ *              Negative: no request in this row; no call reads or writes
+ *              anything else of it.  Above C: FB_ST_BAD_STATE, row left as it is
+ *   tok_pos    [R_max] absolute position of the newest token (what its key is
+ *              rotated by; equal to kv_len - 1 until something is evicted)
+ *   kv_pos     [R_max, n_kv_heads, C] absolute position of every stored key
+ *   kv_weight  [R_max, n_kv_heads, C] fp32, softmax weight that a stored key has
+ *              received so far, summed over the query heads of its KV head
+ *   page_table [R_max, max_pages_per_req]
+ * kv_pos and kv_weight are what fb_evict_kv goes by; a caller that never evicts
+ * may leave both NULL (each KV head has its own because heads evict different
+ * keys).  kv_len may be the prefix_len of an fb_state, page_table its
+ * page_table.  The caller advances kv_len and tok_pos. */
+typedef struct {
+  int32_t* kv_len;
+  int32_t* tok_pos;
+  int32_t* kv_pos;
+  float* kv_weight;
+  int32_t* page_table;
+} fb_cache;
+
+/* Stores the newest token of every request with kv_len >= 1: its K and V (all KV
+ * heads) go to storage position kv_len - 1, kv_pos (if given) becomes tok_pos
+ * and kv_weight (if given) 0 there.  Writes nothing else, so that calling it
+ * again is the same as calling it once.
+ *   k_new, v_new  [R_max, n_kv_heads, head_dim] bf16
+ *   rope_base     as in fb_scatter_window_kv, the angle from tok_pos
+ * A page id outside the pool sets FB_ST_BAD_PAGE and that token is skipped.
+ * fb_append_kv refuses a kv_fp8 context, fb_append_kv_fp8 any other; stored
+ * bytes of 8-bit pages are those of fb_scatter_window_kv_fp8. */
+int fb_append_kv(fb_ctx* ctx, const fb_cache* cache, const void* k_new,
+                 const void* v_new, void* k_pool, void* v_pool,
+                 float rope_base, int32_t* status, void* stream);
+int fb_append_kv_fp8(fb_ctx* ctx, const fb_cache* cache, const void* k_new,
+                     const void* v_new, void* k_pool8, void* v_pool8,
+                     const float* k_scale, const float* v_scale,
+                     float rope_base, int32_t* status, void* stream);
+
 /* One whole step (the four calls above in order) on HOST inputs: copies this
  * step's q / k_win / v_win / logits from host (pinned) memory into the
  * caller's device staging buffers, runs the step, and copies n_committed,

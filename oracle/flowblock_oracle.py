@@ -55,6 +55,12 @@ Pins (tests/test_oracle_*.py, all CPU):
                          values and scale 1 both reduce to the bf16-path
                          functions exactly; dequantised error <= half a code
                          step; scale folded into the scores / the output
+  append_kv              one-block scatter of the same rows; nothing else touched; idempotent
+  token_attn             equal to wavefront_attn's rows on the same keys; closed forms;
+                         permuting the stored keys changes nothing
+  evict_kv               hand-worked case; what stays is what a sort of the whole cache
+                         keeps; the multiset of kept (K, V, position, weight); attention over
+                         the cut cache equals attention with the evicted keys left out
 Nothing in this file is "parity unpinned".
 
 Readings of the paper taken where it is silent or ambiguous are the named
@@ -823,3 +829,102 @@ def serial_blockwise_decode(bl, n_blocks, vocab_mask_id, eos_id, tau_mask,
             blk += 1
             post = 0
     return x, events, step
+
+
+# --------------------------------------------------------------------------
+# Decoding one token at a time over the same pages (no counterpart in the
+# paper, whose serial decoder works block by block).  A cache holds kv_len[r]
+# keys per request, the newest token's included; storage position j of KV head
+# h is page page_table[r, j // page_size], row j % page_size.  A request with
+# kv_len <= 0 has nothing stored, one with kv_len < 0 is no request at all.
+# --------------------------------------------------------------------------
+def append_kv(cfg: Config, kv_len, tok_pos, page_table, k_new, v_new, k_pool, v_pool, kv_pos=None, kv_weight=None,
+              rope_base: float = 0.0, scales=None):
+    """The newest token's K (rotated by tok_pos when rope_base > 0) and V go to
+    storage position kv_len - 1; its position is recorded and its weight is 0.
+    In place.  ``scales`` = (k_scale, v_scale) [Hkv]: the pools are E4M3 bytes."""
+    ps = cfg.page_size
+    for r in range(cfg.max_requests):
+        j = int(kv_len[r]) - 1
+        if j < 0:
+            continue
+        page = int(page_table[r, j // ps])
+        k, v = k_new[r], v_new[r]
+        if rope_base > 0.0:
+            k = rope_rotate(k, int(tok_pos[r]), rope_base)
+        if scales is not None:
+            k = e4m3_quantize(k, np.asarray(scales[0], np.float64)[:, None])
+            v = e4m3_quantize(v, np.asarray(scales[1], np.float64)[:, None])
+        k_pool[page, :, j % ps, :] = k
+        v_pool[page, :, j % ps, :] = v
+        if kv_pos is not None:
+            kv_pos[r, :, j] = tok_pos[r]
+        if kv_weight is not None:
+            kv_weight[r, :, j] = 0.0
+
+
+def stored_rows(cfg: Config, kv_len, page_table, pool, r: int, h: int):
+    """Rows of KV head h that request r has stored, [kv_len, d], in storage order."""
+    ps = cfg.page_size
+    return np.stack([pool[int(page_table[r, j // ps]), h, j % ps] for j in range(int(kv_len[r]))])
+
+
+def token_attn(cfg: Config, kv_len, page_table, q, k_pool, v_pool):
+    """One query token per request over everything it has stored.  q [R, Hq, d],
+    pools in float64 (8-bit pages: decoded and scaled by the caller).  Returns
+    (out [R, Hq, d], w): w[r] is the softmax weight [Hq, kv_len[r]].  Nothing
+    stored: the output is 0."""
+    g = cfg.n_q_heads // cfg.n_kv_heads
+    out = np.zeros(np.shape(q))
+    weights = []
+    for r in range(cfg.max_requests):
+        n = max(0, int(kv_len[r]))
+        w = np.zeros((cfg.n_q_heads, n))
+        for h in range(cfg.n_q_heads if n else 0):
+            k = stored_rows(cfg, kv_len, page_table, k_pool, r, h // g)
+            v = stored_rows(cfg, kv_len, page_table, v_pool, r, h // g)
+            z = _scale(cfg) * (k @ q[r, h])
+            e = np.exp(z - z.max())
+            w[h] = e / e.sum()
+            out[r, h] = w[h] @ v
+        weights.append(w)
+    return out, weights
+
+
+def add_weights(cfg: Config, kv_len, kv_weight, weights):
+    """kv_weight[r, h, j] += softmax weights of the query heads of KV head h."""
+    g = cfg.n_q_heads // cfg.n_kv_heads
+    for r in range(cfg.max_requests):
+        for h in range(cfg.n_kv_heads):
+            for j in range(max(0, int(kv_len[r]))):
+                kv_weight[r, h, j] += weights[r][h * g:(h + 1) * g, j].sum()
+
+
+def evict_kv(cfg: Config, kv_len, tok_pos, kv_pos, kv_weight, page_table, keep, recent: int, sinks: int, k_pool, v_pool):
+    """Cuts every cache of more than keep[r] keys to that many, per KV head.
+    The keys that stay are the first keep[r] in the order: protected ones
+    (position below ``sinks`` or among the last ``recent`` positions) before the
+    others, then greater weight, then lower storage index; a NaN weight ranks
+    below every number.  With n' = keep[r]: the i-th storage index below n' that
+    goes takes over what the i-th index at or above n' that stays holds.  In
+    place; keep[r] < 0: the request is left alone."""
+    ps = cfg.page_size
+    for r in range(cfg.max_requests):
+        n, m = int(kv_len[r]), int(keep[r])
+        if n <= 0 or m < 0 or n <= m:
+            continue
+        for h in range(cfg.n_kv_heads):
+            def rank(j):
+                p, w = int(kv_pos[r, h, j]), float(kv_weight[r, h, j])
+                safe = p < sinks or p > int(tok_pos[r]) - recent
+                return (not safe, np.isnan(w), 0.0 if np.isnan(w) else -w, j)
+            stays = sorted(sorted(range(n), key=rank)[:m])
+            holes = [j for j in range(m) if j not in set(stays)]
+            above = [j for j in stays if j >= m]
+            for to, at in zip(holes, above):
+                pt, pa = int(page_table[r, to // ps]), int(page_table[r, at // ps])
+                k_pool[pt, h, to % ps] = k_pool[pa, h, at % ps]
+                v_pool[pt, h, to % ps] = v_pool[pa, h, at % ps]
+                kv_pos[r, h, to] = kv_pos[r, h, at]
+                kv_weight[r, h, to] = kv_weight[r, h, at]
+        kv_len[r] = m

@@ -32,7 +32,8 @@ EXPORTS = ["fb_create", "fb_destroy", "fb_last_error", "fb_workspace_bytes",
            "fb_gate_commit", "fb_step_host", "fb_wavefront_attn_static",
            "fb_scatter_window_kv", "fb_embed_gather", "fb_lm_head_t2t",
            "fb_lm_head_workspace_bytes", "fb_set_tuning", "fb_attn_plan_host",
-           "fb_scatter_window_kv_fp8", "fb_wavefront_attn_fp8"]
+           "fb_scatter_window_kv_fp8", "fb_wavefront_attn_fp8", "fb_append_kv",
+           "fb_append_kv_fp8"]
 
 
 class fb_config(C.Structure):
@@ -65,6 +66,11 @@ class fb_pack(C.Structure):
         "slot_flags", "req_slot_begin", "qtok", "pos")]
 
 
+class fb_cache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in (
+        "kv_len", "tok_pos", "kv_pos", "kv_weight", "page_table")]
+
+
 class fb_host_io(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in (
         "h_q", "h_k_win", "h_v_win", "h_logits", "h_n_committed", "h_spawned",
@@ -81,7 +87,7 @@ class fb_device_bufs(C.Structure):
 # the calls that _marshal makes, in the order of its bind()
 _FAST = ("fb_pack_wavefronts", "fb_wavefront_attn", "fb_t2t_step", "fb_gate_commit", "fb_scatter_window_kv",
          "fb_scatter_window_kv_fp8", "fb_wavefront_attn_fp8", "fb_embed_gather", "fb_lm_head_t2t",
-         "fb_wavefront_attn_static")
+         "fb_wavefront_attn_static", "fb_append_kv", "fb_append_kv_fp8")
 
 _lib = None
 _m = None
@@ -126,6 +132,8 @@ def lib() -> C.CDLL:
         l.fb_lm_head_workspace_bytes.restype = C.c_size_t
         l.fb_lm_head_t2t.argtypes = [P, C.POINTER(fb_pack), P, P, C.c_int32,
                                      C.POINTER(fb_state)] + [P] * 7
+        l.fb_append_kv.argtypes = [P, C.POINTER(fb_cache)] + [P] * 4 + [C.c_float, P, P]
+        l.fb_append_kv_fp8.argtypes = [P, C.POINTER(fb_cache)] + [P] * 6 + [C.c_float, P, P]
         l.fb_step_host.argtypes = [P, C.POINTER(fb_state), C.POINTER(fb_pack),
                                    C.POINTER(fb_device_bufs),
                                    C.POINTER(fb_host_io), P]
@@ -138,6 +146,7 @@ def lib() -> C.CDLL:
         except ImportError as e:
             raise RuntimeError("the marshalling module has not been built for this Python; run "
                                "`python -m paper_2607_17652_b200.build`") from e
+        _marshal.dtypes(torch.int32, torch.float32, torch.bfloat16, torch.uint8)
         _marshal.bind(*(C.cast(getattr(l, n), P).value for n in _FAST))
         _lib, _m = l, _marshal
     return _lib
@@ -171,6 +180,10 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _device() -> int:
+    return _raw_device() if _raw_device is not None else torch.cuda.current_device()
+
+
 class Context:
     """Owns one fb_ctx.  ``tuning``: optional dict of fb_tuning fields."""
 
@@ -181,6 +194,11 @@ class Context:
         if rc != FB_OK:
             raise FlowBlockError(rc, lib().fb_last_error(None).decode())
         self._hv = self._h.value
+        # what the calls that decode one token at a time hold their tensors against (csrc/marshal.c)
+        c = self.cfg
+        R, H, P = c.max_requests, c.n_kv_heads, c.max_pages_per_req
+        self._sizes = (R, R * H * P * c.page_size, R * P, R * H * c.head_dim, R * c.n_q_heads * c.head_dim,
+                       c.num_pages * H * c.page_size * c.head_dim, H)
         if tuning:
             self.set_tuning(**tuning)
 
@@ -277,6 +295,32 @@ class PackBuffers:
         return {n: getattr(self, n).cpu().numpy() for n, _ in fb_pack._fields_}
 
 
+@dataclass
+class CacheState:
+    """What the calls that decode one token at a time know of the caches (fb_cache): lengths, positions and
+    weights of what is stored.  ``kv_pos`` and ``kv_weight`` may be None where nothing is ever evicted."""
+    kv_len: torch.Tensor
+    tok_pos: torch.Tensor
+    kv_pos: torch.Tensor | None
+    kv_weight: torch.Tensor | None
+    page_table: torch.Tensor
+
+    @classmethod
+    def alloc(cls, ctx: Context, device, page_table, records: bool = True):
+        """No request in any row (kv_len -1); ``records``: with positions and weights."""
+        c = ctx.cfg
+        cells = (c.max_requests, c.n_kv_heads, c.max_pages_per_req * c.page_size)
+        z = lambda shape, dt=torch.int32: torch.zeros(shape, dtype=dt, device=device)
+        return cls(z(c.max_requests) - 1, z(c.max_requests), z(cells) if records else None,
+                   z(cells, torch.float32) if records else None, page_table)
+
+    def c(self) -> fb_cache:
+        return fb_cache(*(_ptr(getattr(self, n)) for n, _ in fb_cache._fields_))
+
+    def to_numpy(self):
+        return {n: getattr(self, n).cpu().numpy() for n, _ in fb_cache._fields_ if getattr(self, n) is not None}
+
+
 def alloc_workspace(ctx: Context, device) -> torch.Tensor:
     n = ctx.workspace_bytes()
     return torch.zeros((n + 255) // 256 * 256, dtype=torch.uint8, device=device)
@@ -363,6 +407,23 @@ def fb_gate_commit(ctx: Context, pk: PackBuffers, slot_stats, st: DeviceState,
                    step_counters, status, stream=None):
     rc = _m.gate(ctx._hv, pk, slot_stats, st, k_win, v_win, k_pool, v_pool, n_committed, spawned, step_counters, status,
                  _stream(stream))
+    if rc:
+        ctx.check(rc)
+
+
+def fb_append_kv(ctx: Context, cache: CacheState, k_new, v_new, k_pool, v_pool, status, rope_base: float = 0.0,
+                 stream=None):
+    """The newest token's K and V of every request to storage position kv_len - 1."""
+    rc = _m.append(ctx._hv, ctx._sizes, _device(), cache, k_new, v_new, k_pool, v_pool, rope_base, status, _stream(stream))
+    if rc:
+        ctx.check(rc)
+
+
+def fb_append_kv_fp8(ctx: Context, cache: CacheState, k_new, v_new, k_pool8, v_pool8, k_scale, v_scale, status,
+                     rope_base: float = 0.0, stream=None):
+    """The same into 8-bit (E4M3) pages."""
+    rc = _m.append_fp8(ctx._hv, ctx._sizes, _device(), cache, k_new, v_new, k_pool8, v_pool8, rope_base, status,
+                       _stream(stream), k_scale, v_scale)
     if rc:
         ctx.check(rc)
 

@@ -372,6 +372,44 @@ int fb_gate_commit(fb_ctx* ctx, const fb_pack* pk, const int32_t* slot_stats, co
                          step_counters, status, (cudaStream_t)stream);
 }
 
+// What the calls that decode one token at a time have in common.  Capacities past 2^31 - 1 positions are refused:
+// lengths and positions are int32.
+static int check_cache(fb_ctx* ctx, const fb_cache* kv, int fp8) {
+  if (!kv) return fail(ctx, FB_ERR_INVALID_ARG, "cache is null");
+  if (!kv->kv_len || !kv->page_table) return fail(ctx, FB_ERR_INVALID_ARG, "cache.kv_len or cache.page_table is null");
+  if (fp8 >= 0 && fp8 != ctx->cfg.kv_fp8)
+    return fail(ctx, FB_ERR_UNSUPPORTED, fp8 ? "8-bit KV pages need a context created with kv_fp8 = 1 (window_in_pages = 1, head_dim = 128)"
+                                             : "this context holds 8-bit pages: use the call whose name ends in _fp8");
+  if ((long long)ctx->cfg.max_pages_per_req * fb::kPage > 0x7fffffffll)
+    return fail(ctx, FB_ERR_UNSUPPORTED, "max_pages_per_req * 64 must be below 2^31");
+  return FB_OK;
+}
+
+static int append(fb_ctx* ctx, const fb_cache* kv, const void* k_new, const void* v_new, void* k_pool, void* v_pool,
+                  const float* k_scale, const float* v_scale, int fp8, float rope_base, int32_t* status, void* stream) {
+  if (!ctx) return fail(nullptr, FB_ERR_INVALID_ARG, "ctx is null");
+  if (int e = check_cache(ctx, kv, fp8)) return e;
+  if (!kv->tok_pos) return fail(ctx, FB_ERR_INVALID_ARG, "cache.tok_pos is null");
+  if (!k_new || !v_new || !k_pool || !v_pool || !status || (fp8 && (!k_scale || !v_scale)))
+    return fail(ctx, FB_ERR_INVALID_ARG, "a tensor pointer is null");
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pool) || !aligned16(v_pool))
+    return fail(ctx, FB_ERR_ALIGNMENT, "tensor pointers must be 16-byte aligned");
+  if (!(rope_base == rope_base) || rope_base < 0.f) return fail(ctx, FB_ERR_INVALID_ARG, "rope_base is NaN or negative");
+  return fb::launch_append(ctx, kv, k_new, v_new, k_pool, v_pool, k_scale, v_scale, rope_base, status,
+                           (cudaStream_t)stream);
+}
+
+int fb_append_kv(fb_ctx* ctx, const fb_cache* cache, const void* k_new, const void* v_new, void* k_pool, void* v_pool,
+                 float rope_base, int32_t* status, void* stream) {
+  return append(ctx, cache, k_new, v_new, k_pool, v_pool, nullptr, nullptr, 0, rope_base, status, stream);
+}
+
+int fb_append_kv_fp8(fb_ctx* ctx, const fb_cache* cache, const void* k_new, const void* v_new, void* k_pool8,
+                     void* v_pool8, const float* k_scale, const float* v_scale, float rope_base, int32_t* status,
+                     void* stream) {
+  return append(ctx, cache, k_new, v_new, k_pool8, v_pool8, k_scale, v_scale, 1, rope_base, status, stream);
+}
+
 int fb_step_host(fb_ctx* ctx, const fb_state* st, const fb_pack* pk, const fb_device_bufs* dev,
                  const fb_host_io* io, void* stream) {
   if (!ctx) return fail(nullptr, FB_ERR_INVALID_ARG, "ctx is null");

@@ -267,6 +267,8 @@ struct fb_ctx {
   float sm_scale;
   fb::WsLayout ws;
   std::string err;
+  float rope_base = 0.f;       // the base whose frequencies these are
+  double inv_freq[64] = {};
   // lazily initialised at the first attention launch
   bool dev_ready = false;
   int device = -1;        // the device the lazily initialised members belong to
@@ -350,6 +352,8 @@ size_t lm_head_workspace_bytes(const fb_ctx*);
 int lm_head_device_setup(fb_ctx*);
 int launch_embed(fb_ctx*, const fb_pack*, const void* table, int table_rows, int hidden, void* x,
                  int32_t* status, cudaStream_t);
+int launch_append(fb_ctx*, const fb_cache*, const void* k_new, const void* v_new, void* k_pool, void* v_pool,
+                  const float* k_scale, const float* v_scale, float rope_base, int32_t* status, cudaStream_t);
 int launch_t2t(fb_ctx*, const fb_pack*, const void* logits, const fb_state*, int32_t* argmax,
                float* conf, uint8_t* action, int32_t* slot_stats, int32_t* status, cudaStream_t);
 int launch_gate(fb_ctx*, const fb_pack*, const int32_t* slot_stats, const fb_state*,
