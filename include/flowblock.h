@@ -460,6 +460,35 @@ int fb_append_kv_fp8(fb_ctx* ctx, const fb_cache* cache, const void* k_new,
                      const float* k_scale, const float* v_scale,
                      float rope_base, int32_t* status, void* stream);
 
+/* One query token per request over everything the request has stored: for every
+ * row with kv_len >= 0 and every query head, softmax(sm_scale * q k^T) v over
+ * storage positions [0, kv_len).  Storage positions behind kv_len are not read
+ * (they may hold anything).  kv_len = 0: the output row is 0.  Keys of a page
+ * outside the pool are left out and FB_ST_BAD_PAGE is set.
+ *   q, out      [R_max, n_q_heads, head_dim] bf16; rows of kv_len < 0 are not
+ *               written
+ *   accumulate  0, or 1: kv_weight[r, h, j] += the sum over the query heads of KV
+ *               head h of the softmax weights of key j (fp32; each row is added
+ *               by one thread in a fixed order, so that results repeat bit for
+ *               bit).  A call with accumulate = 1 whose output nobody uses weighs
+ *               the keys by any query of the caller's
+ *   ws          fb_token_workspace_bytes(ctx, accumulate) bytes of device scratch,
+ *               256-byte aligned; nothing in it outlives the call.  Calls that
+ *               overlap on the device need workspaces of their own
+ * fp32 scores, statistics and sums; the softmax weights are rounded to the 16-bit
+ * type of the second product (bf16; fp16 where the pages hold 8 bits), the
+ * output to bf16.  8-bit pages: K and V are taken as byte * scale exactly, the
+ * queries as fp16 after an exact power-of-two scaling per row. */
+size_t fb_token_workspace_bytes(const fb_ctx* ctx, int32_t accumulate);
+int fb_token_attn(fb_ctx* ctx, const fb_cache* cache, const void* q,
+                  const void* k_pool, const void* v_pool, void* out,
+                  int32_t accumulate, void* ws, int32_t* status, void* stream);
+int fb_token_attn_fp8(fb_ctx* ctx, const fb_cache* cache, const void* q,
+                      const void* k_pool8, const void* v_pool8,
+                      const float* k_scale, const float* v_scale, void* out,
+                      int32_t accumulate, void* ws, int32_t* status,
+                      void* stream);
+
 /* One whole step (the four calls above in order) on HOST inputs: copies this
  * step's q / k_win / v_win / logits from host (pinned) memory into the
  * caller's device staging buffers, runs the step, and copies n_committed,

@@ -410,6 +410,39 @@ int fb_append_kv_fp8(fb_ctx* ctx, const fb_cache* cache, const void* k_new, cons
   return append(ctx, cache, k_new, v_new, k_pool8, v_pool8, k_scale, v_scale, 1, rope_base, status, stream);
 }
 
+size_t fb_token_workspace_bytes(const fb_ctx* ctx, int32_t accumulate) {
+  return ctx ? fb::token_workspace_bytes(ctx, accumulate != 0) : 0;
+}
+
+static int token_attn(fb_ctx* ctx, const fb_cache* kv, const void* q, const void* k_pool, const void* v_pool,
+                      const float* k_scale, const float* v_scale, int fp8, void* out, int32_t accumulate, void* ws,
+                      int32_t* status, void* stream) {
+  if (!ctx) return fail(nullptr, FB_ERR_INVALID_ARG, "ctx is null");
+  if (int e = check_cache(ctx, kv, fp8)) return e;
+  if (accumulate != 0 && accumulate != 1) return fail(ctx, FB_ERR_INVALID_ARG, "accumulate must be 0 or 1");
+  if (accumulate && !kv->kv_weight) return fail(ctx, FB_ERR_INVALID_ARG, "cache.kv_weight is null");
+  if (!q || !k_pool || !v_pool || !out || (fp8 && (!k_scale || !v_scale)))
+    return fail(ctx, FB_ERR_INVALID_ARG, "a tensor pointer is null");
+  if (!ws) return fail(ctx, FB_ERR_WORKSPACE, "workspace is null");
+  if (!status) return fail(ctx, FB_ERR_INVALID_ARG, "status is null");
+  if (!aligned16(q) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(out))
+    return fail(ctx, FB_ERR_ALIGNMENT, "tensor pointers must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(ctx, FB_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
+  return fb::launch_token_attn(ctx, kv, q, k_pool, v_pool, k_scale, v_scale, out, accumulate, ws, status,
+                               (cudaStream_t)stream);
+}
+
+int fb_token_attn(fb_ctx* ctx, const fb_cache* cache, const void* q, const void* k_pool, const void* v_pool, void* out,
+                  int32_t accumulate, void* ws, int32_t* status, void* stream) {
+  return token_attn(ctx, cache, q, k_pool, v_pool, nullptr, nullptr, 0, out, accumulate, ws, status, stream);
+}
+
+int fb_token_attn_fp8(fb_ctx* ctx, const fb_cache* cache, const void* q, const void* k_pool8, const void* v_pool8,
+                      const float* k_scale, const float* v_scale, void* out, int32_t accumulate, void* ws,
+                      int32_t* status, void* stream) {
+  return token_attn(ctx, cache, q, k_pool8, v_pool8, k_scale, v_scale, 1, out, accumulate, ws, status, stream);
+}
+
 int fb_step_host(fb_ctx* ctx, const fb_state* st, const fb_pack* pk, const fb_device_bufs* dev,
                  const fb_host_io* io, void* stream) {
   if (!ctx) return fail(nullptr, FB_ERR_INVALID_ARG, "ctx is null");

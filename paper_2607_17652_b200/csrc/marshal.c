@@ -26,7 +26,7 @@ static const char* const k_pack[9] = {"n_live", "slot_req", "slot_s", "slot_pos0
 
 /* entry points, in the order of `names` in bind() */
 enum { F_PACK, F_ATTN, F_T2T, F_GATE, F_SCATTER, F_SCATTER8, F_ATTN8, F_EMBED, F_HEAD, F_STATIC,
-       F_APPEND, F_APPEND8, F_COUNT };
+       F_APPEND, F_APPEND8, F_TOKEN, F_TOKEN8, F_COUNT };
 static void* fn[F_COUNT];
 
 static PyObject* bind(PyObject* self, PyObject* const* args, Py_ssize_t n) {
@@ -202,8 +202,8 @@ static PyObject* m_static(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 }
 
 /* `sizes` of a context, in elements (binding.Context): requests, records, page table, a K or V row a request, a q row a
- * request, a pool, KV heads */
-enum { Z_REQ, Z_REC, Z_PT, Z_KV, Z_Q, Z_POOL, Z_HEADS, Z_COUNT };
+ * request, a pool, KV heads, bytes of workspace of the attention without and with weights */
+enum { Z_REQ, Z_REC, Z_PT, Z_KV, Z_Q, Z_POOL, Z_HEADS, Z_WS, Z_WS_WEIGHTS, Z_COUNT };
 static int as_sizes(PyObject* o, long long* z) {
   if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != Z_COUNT) { PyErr_SetString(PyExc_TypeError, "sizes"); return -1; }
   for (int i = 0; i < Z_COUNT; ++i)
@@ -250,11 +250,33 @@ static PyObject* append(PyObject* self, PyObject* const* a, Py_ssize_t n, int fp
 static PyObject* m_append(PyObject* self, PyObject* const* a, Py_ssize_t n) { return append(self, a, n, 0); }
 static PyObject* m_append8(PyObject* self, PyObject* const* a, Py_ssize_t n) { return append(self, a, n, 1); }
 
+/* handle, sizes, device, cache, q, k_pool, v_pool, out, accumulate, ws, status, stream[, k_scale, v_scale] */
+static PyObject* token(PyObject* self, PyObject* const* a, Py_ssize_t n, int fp8) {
+  ARGS(fp8 ? 14 : 12, "token_attn") CACHE("fb_token_attn")
+  int32_t accumulate;
+  if (as_int(a[8], &accumulate)) return NULL;
+  TENSOR(q, 4, "fb_token_attn", "q", T_BF16, z[Z_Q], 0)
+  TENSOR(kp, 5, "fb_token_attn", "k_pool", fp8 ? T_U8 : T_BF16, z[Z_POOL], 1)
+  TENSOR(vp, 6, "fb_token_attn", "v_pool", fp8 ? T_U8 : T_BF16, z[Z_POOL], 1)
+  TENSOR(out, 7, "fb_token_attn", "out", T_BF16, z[Z_Q], 0)
+  TENSOR(ws, 9, "fb_token_attn", "ws", T_U8, z[accumulate ? Z_WS_WEIGHTS : Z_WS], 1)
+  TENSOR(status, 10, "fb_token_attn", "status", T_I32, 1, 1)
+  void *ks = NULL, *vs = NULL, *stream;
+  if (fp8 && (as_tensor(a[12], "fb_token_attn", "k_scale", T_F32, z[Z_HEADS], 0, dev, &ks) ||
+              as_tensor(a[13], "fb_token_attn", "v_scale", T_F32, z[Z_HEADS], 0, dev, &vs))) return NULL;
+  if (as_ptr(a[11], &stream)) return NULL;
+  if (fp8) { CALL(FN(F_TOKEN8, fb_token_attn_fp8)(ctx, &kv, q, kp, vp, ks, vs, out, accumulate, ws, status, stream)) }
+  CALL(FN(F_TOKEN, fb_token_attn)(ctx, &kv, q, kp, vp, out, accumulate, ws, status, stream))
+}
+static PyObject* m_token(PyObject* self, PyObject* const* a, Py_ssize_t n) { return token(self, a, n, 0); }
+static PyObject* m_token8(PyObject* self, PyObject* const* a, Py_ssize_t n) { return token(self, a, n, 1); }
+
 #define M(name, f) {name, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {
     M("bind", bind), M("pack", m_pack), M("attn", m_attn), M("attn_fp8", m_attn8), M("t2t", m_t2t), M("gate", m_gate),
     M("scatter", m_scatter), M("scatter_fp8", m_scatter8), M("embed", m_embed), M("lm_head", m_head),
-    M("attn_static", m_static), M("dtypes", dtypes), M("append", m_append), M("append_fp8", m_append8), {NULL, NULL, 0, NULL}};
+    M("attn_static", m_static), M("dtypes", dtypes), M("append", m_append), M("append_fp8", m_append8),
+    M("token_attn", m_token), M("token_attn_fp8", m_token8), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the binding", -1, methods,
                                     NULL, NULL, NULL, NULL};
 

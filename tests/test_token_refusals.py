@@ -103,3 +103,55 @@ def test_tensors_of_another_type_size_stride_or_device_are_refused(monkeypatch):
     monkeypatch.setattr(B, "_device", lambda: 0)       # tensors elsewhere than on the current device
     with pytest.raises(ValueError, match="device 0"):
         B.fb_append_kv(ctx, cache_tensors(), t["k"], t["v"], t["pool"], t["pool"], t["status"])
+
+
+def test_token_attn_refuses():
+    lib, ctx, ctx8 = B.lib(), B.Context(**GOOD), B.Context(**FP8)
+    call = lambda c, kv, *a: lib.fb_token_attn(c.handle, kv and C.byref(kv), *a)
+    ok = [P, P, P, P, 0, P, P, None]               # q, k_pool, v_pool, out, accumulate, ws, status, stream
+    refused(ctx, call(ctx, None, *ok), B.FB_ERR_INVALID_ARG, b"cache is null")
+    for name in ("kv_len", "page_table"):
+        refused(ctx, call(ctx, with_null(name), *ok), B.FB_ERR_INVALID_ARG, b"cache.kv_len or cache.page_table")
+    for i in (0, 1, 2, 3, 6):
+        a = list(ok)
+        a[i] = None
+        refused(ctx, call(ctx, full(), *a), B.FB_ERR_INVALID_ARG, b"null")
+    a = list(ok)
+    a[5] = None
+    refused(ctx, call(ctx, full(), *a), B.FB_ERR_WORKSPACE, b"workspace is null")
+    for i in (0, 1, 2, 3, 5):
+        a = list(ok)
+        a[i] = P + 8
+        refused(ctx, call(ctx, full(), *a), B.FB_ERR_ALIGNMENT, b"aligned")
+    for acc in (2, -1):
+        a = list(ok)
+        a[4] = acc
+        refused(ctx, call(ctx, full(), *a), B.FB_ERR_INVALID_ARG, b"accumulate")
+    a[4] = 1
+    refused(ctx, call(ctx, with_null("kv_weight"), *a), B.FB_ERR_INVALID_ARG, b"kv_weight")
+    refused(ctx8, call(ctx8, full(), *ok), B.FB_ERR_UNSUPPORTED, b"_fp8")
+    call8 = lambda c, *b: lib.fb_token_attn_fp8(c.handle, C.byref(full()), *b)
+    ok8 = [P, P, P, P, P, P, 0, P, P, None]
+    refused(ctx, call8(ctx, *ok8), B.FB_ERR_UNSUPPORTED, b"kv_fp8 = 1")
+    refused(ctx8, call8(ctx8, P, P, P, P, None, P, 0, P, P, None), B.FB_ERR_INVALID_ARG, b"null")
+    assert lib.fb_token_attn(None, None, *ok) == B.FB_ERR_INVALID_ARG
+    assert lib.fb_token_workspace_bytes(None, 0) == 0
+    assert lib.fb_token_workspace_bytes(ctx.handle, 1) >= lib.fb_token_workspace_bytes(ctx.handle, 0) > 0
+
+
+def test_token_attn_refuses_tensors_that_do_not_fit(monkeypatch):
+    ctx, t = B.Context(**GOOD), tensors()
+    monkeypatch.setattr(B, "_device", lambda: -1)
+    monkeypatch.setattr(B, "_stream", lambda s: 0)
+    q = torch.zeros(4, 8, 128, dtype=torch.bfloat16)
+    ws = [B.alloc_token_workspace(ctx, "cpu", a) for a in (False, True)]
+    bad = [dict(q=q[:3]), dict(q=q.half()), dict(q=q.transpose(0, 1)), dict(out=q.float()), dict(out=q[:, ::2]),
+           dict(ws=ws[0][:-1].clone()), dict(ws=ws[1][:-1].clone(), acc=True), dict(pool=t["pool"][:8]), dict(status=t["status"].long())]
+    for b in bad:
+        u = dict(dict(q=q, out=q.clone(), ws=ws[1], pool=t["pool"], status=t["status"], acc=False), **b)
+        if "ws" in b and not u["acc"] and b["ws"].numel() >= B.lib().fb_token_workspace_bytes(ctx.handle, 0):
+            u["ws"] = torch.zeros(8, dtype=torch.uint8)
+        if "ws" in b and u["acc"] and b["ws"].numel() >= B.lib().fb_token_workspace_bytes(ctx.handle, 1):
+            u["ws"] = torch.zeros(8, dtype=torch.uint8)
+        with pytest.raises(ValueError, match="contiguous"):
+            B.fb_token_attn(ctx, cache_tensors(), u["q"], u["pool"], u["pool"], u["out"], u["ws"], u["status"], u["acc"])

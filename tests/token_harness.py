@@ -89,7 +89,9 @@ class Case:
         return cache, self.k_pool.to(dev), self.v_pool.to(dev)
 
     def dev_scales(self, dev="cuda:0"):
-        return [s.to(dev) for s in self.scales]
+        if not hasattr(self, "_dev_scales"):
+            self._dev_scales = [s.to(dev) for s in self.scales]
+        return self._dev_scales
 
 
 def bits(t: torch.Tensor) -> np.ndarray:
