@@ -6,9 +6,11 @@
 //
 // Work.  The keys of a (request, KV head) are cut into tiles, and the tiles of the whole batch, one row behind the
 // other, are dealt to the CTAs in equal contiguous shares, whatever the lengths: a row that a CTA holds whole is
-// finished by it, one that is cut leaves a piece (reference, sum, unnormalised output) per CTA, and
-// token_join_kernel adds the pieces in order.  A CTA starts at most one row that it does not finish and finishes at
-// most one that it did not start, so two slots a CTA hold all pieces, however large the batch.
+// finished by it, one that is cut leaves a piece (reference, sum, unnormalised output) per CTA, and token_join_kernel
+// adds the pieces in their order.  A CTA starts at most one row that it does not finish and finishes at most one that it
+// did not start, so two slots a CTA hold all pieces, however large the batch.  (Adding them in the CTA that finds all
+// pieces of a row there saves the launch, and its fences and polls cost more than the launch boundary: one request of
+// 3,001 keys 9.8 -> 13.0 us, 24 requests 20.6 -> 23.6.)
 //
 // A warp has 16 keys of a tile (32 where a row is 128 bytes) and works alone until its share ends:
 //   S^T = K Q^T   (m16n8k16: 16 keys, 8 query heads; padded to 8)   and   O^T += V^T P^T  (16 of d, 8 heads)
@@ -32,19 +34,21 @@ constexpr float kTokLog2e = 1.4426950408889634f;
 constexpr float kNoRef = -3.0e38f;       // below every score: the reference of a row that has seen no key
 constexpr float kRebase = 8.f;           // a score that far (in powers of two) above the reference moves it
 
+using bf16 = __nv_bfloat16;
+
 struct TokenParams {
   const int32_t *kv_len, *page_table;
   float* kv_weight;
-  const __nv_bfloat16* q;
+  const bf16* q;
   const char *k_pool, *v_pool;
   const float *k_scale, *v_scale;        // 8-bit pages: [n_kv_heads]
-  __nv_bfloat16* out;
+  bf16* out;
   int32_t* status;
   float* part_o;                         // [2 n_ctas][heads of a block][d] unnormalised outputs of the pieces
   float2* part_ml;                       // [2 n_ctas][heads of a block] reference (log2), sum
-  float2* row_ml;                        // [rows][heads of a block] the same of rows that were not cut (weights only)
+  float2* row_ml;                        // [rows][heads of a block] reference and sum of rows that were not cut (weights only)
   float* scores;                         // [requests][KV heads][capacity][group] (log2; weights only)
-  int32_t requests, group, n_kv_heads, head_blocks, max_pages_per_req, num_pages, n_ctas;
+  int32_t requests, group, n_kv_heads, head_blocks, max_pages_per_req, num_pages, n_ctas, join_ctas;
   float sm_scale;
 };
 
@@ -85,81 +89,97 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-// two E4M3 bytes -> two fp16 (exact)
-__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
-  uint32_t r;
-  asm("{\n\t.reg .b16 t;\n\tcvt.u16.u32 t, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, t;\n\t}" : "=r"(r) : "r"(two));
-  return r;
+// four E4M3 bytes -> two pairs of fp16 (exact)
+__device__ __forceinline__ void e4m3x4_to_f16(uint32_t four, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(lo), "=r"(hi) : "r"(four));
 }
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 // ---------------------------------------------------------------- the deal
-// Tiles of request r (none where there is no request, nothing stored or the length is no length).
-__device__ __forceinline__ int tok_tiles(const TokenParams& p, int r, int tile) {
-  const int len = r < p.requests ? __ldcg(p.kv_len + r) : 0;
+// Tiles of `len` stored keys (none where there is no request, nothing stored or the length is no length).
+__device__ __forceinline__ int tok_tiles(const TokenParams& p, int len, int tile) {
   return len > 0 && len <= (long long)p.max_pages_per_req * kPage ? (len + tile - 1) / tile : 0;
 }
-__device__ __forceinline__ long long warp_sum(long long v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-// Tiles of all rows, and of those of the requests before `upto`.  By a whole warp.
-__device__ __forceinline__ long long tok_total(const TokenParams& p, int tile, int upto, long long& before) {
-  long long all = 0, b = 0;
-  for (int r0 = 0; r0 < p.requests; r0 += 32) {
-    const int r = r0 + (threadIdx.x & 31), n = tok_tiles(p, r, tile);
+__device__ __forceinline__ int tok_len(const TokenParams& p, int r) { return r < p.requests ? __ldcg(p.kv_len + r) : 0; }
+// Tiles of all rows (`total`) and of those of the requests before `upto`, and the share of a CTA: an equal one, but no
+// row in more than kMostPieces.  By a whole warp; `len`: the lane's length of the first 32 requests.
+constexpr int kMostPieces = 64;
+struct TokDeal { long long total, before, share; };
+__device__ __forceinline__ TokDeal tok_deal(const TokenParams& p, int tile, int len, int upto) {
+  const int lane = threadIdx.x & 31, rows = p.n_kv_heads * p.head_blocks;
+  int longest = tok_tiles(p, len, tile);
+  long long all = longest, before = lane < upto ? longest : 0;
+#pragma unroll 4
+  for (int r = 32 + lane; r < p.requests; r += 32) {
+    const int n = tok_tiles(p, __ldcg(p.kv_len + r), tile);
     all += n;
-    b += r < upto ? n : 0;
+    before += r < upto ? n : 0;
+    longest = max(longest, n);
   }
-  const int rows = p.n_kv_heads * p.head_blocks;
-  before = warp_sum(b) * rows;
-  return warp_sum(all) * rows;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    all += __shfl_xor_sync(0xffffffffu, all, o);
+    before += __shfl_xor_sync(0xffffffffu, before, o);
+  }
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  TokDeal d;
+  d.total = all * rows;
+  d.before = before * rows;
+  d.share = max((d.total + p.n_ctas - 1) / p.n_ctas, (long long)((longest + kMostPieces - 1) / kMostPieces));
+  return d;
 }
-__device__ __forceinline__ long long tok_share(long long total, int n_ctas) {
-  const long long s = (total + n_ctas - 1) / n_ctas;
-  return s < 1 ? 1 : s;
-}
+// The pieces of a row: CTAs c0.. of the deal; a piece lies in slot 2 c + 1 where the row starts in that CTA, else in 2 c.
+struct TokPieces {
+  long long start, share;
+  int c0, n;
+  __device__ __forceinline__ TokPieces(long long start_, int nt, long long share_) : start(start_), share(share_) {
+    c0 = (int)(start / share);
+    n = (int)((start + nt - 1) / share) - c0 + 1;
+  }
+  __device__ __forceinline__ int slot(int i) const { return 2 * (c0 + i) + ((c0 + i) * share <= start ? 1 : 0); }
+};
 
 // ---------------------------------------------------------------- the stream
 template <int D, bool F8, int NB, bool W>
 __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kernel(const TokenParams p) {
   using S = TokShape<D, F8>;
   constexpr int HB = 8 * NB, kStride = D + 1;
-  constexpr float kShift = F8 ? 7.f : 0.f;     // fp16 weights: 2^7 above 1, so that 2^-31 of the reference is still there
+  constexpr float kShift = F8 ? 7.f : 0.f;     // fp16 weights start 2^7 above 1 (the reference lies that far below), so that 2^-31 is still there
   __shared__ float sh_o[kTokWarps][HB * kStride];
   __shared__ float2 sh_ml[kTokWarps][HB];
   pdl_wait_then_release();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c = lane >> 2, t = lane & 3;
-  long long unused;
-  const long long total = tok_total(p, S::kTile, 0, unused), share = tok_share(total, p.n_ctas);
-  long long at = (long long)blockIdx.x * share;
-  int left = (int)min(share, total - at > 0 ? total - at : 0);
+  const int rows = p.n_kv_heads * p.head_blocks;
+  int len = tok_len(p, lane);
+  const TokDeal deal = tok_deal(p, S::kTile, len, 0);
+  long long at = (long long)blockIdx.x * deal.share;
+  int left = (int)min(deal.share, deal.total - at > 0 ? deal.total - at : 0);
   // rows without work: zeros where nothing is stored, a report where the length is no length
   for (int r = blockIdx.x; r < p.requests; r += p.n_ctas) {
-    const int len = __ldcg(p.kv_len + r);
-    if (len > (long long)p.max_pages_per_req * kPage && tid == 0) atomicOr(p.status, FB_ST_BAD_STATE);
-    if (len != 0) continue;
+    const int n = __ldcg(p.kv_len + r);
+    if (n > (long long)p.max_pages_per_req * kPage && tid == 0) atomicOr(p.status, FB_ST_BAD_STATE);
+    if (n != 0) continue;
     uint4* o = reinterpret_cast<uint4*>(p.out) + (size_t)r * p.n_kv_heads * p.group * (D / 8);
     for (int i = tid; i < p.n_kv_heads * p.group * (D / 8); i += kTokThreads) o[i] = make_uint4(0, 0, 0, 0);
   }
   if (left <= 0) return;
-  // the request that holds tile `at`
-  const int rows = p.n_kv_heads * p.head_blocks;
+  // the request that holds tile `at`, its length and tiles
   int r = 0, nt = 0;
   for (int r0 = 0; r0 < p.requests; r0 += 32) {
-    const int n = tok_tiles(p, r0 + lane, S::kTile);
+    if (r0 > 0) len = tok_len(p, r0 + lane);
+    const int n = tok_tiles(p, len, S::kTile);
     int incl = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int v = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += v;
     }
-    const long long end = (long long)incl * rows;
-    const unsigned here = __ballot_sync(0xffffffffu, at < end);
+    const unsigned here = __ballot_sync(0xffffffffu, at < (long long)incl * rows);
     if (here) {
       const int l = __ffs(here) - 1;
       nt = __shfl_sync(0xffffffffu, n, l);
+      len = __shfl_sync(0xffffffffu, len, l);
       at -= (long long)(__shfl_sync(0xffffffffu, incl, l) - nt) * rows;
       r = r0 + l;
       break;
@@ -171,9 +191,43 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
 
   while (true) {
     const int h = row / p.head_blocks, hb = row % p.head_blocks;
-    const int len = __ldcg(p.kv_len + r);
     const int seg = min(left, nt - tile), tile_end = tile + seg;
-    const int32_t* pages = p.page_table + (size_t)r * p.max_pages_per_req;
+    // Steps of this warp: `rem` keys are stored from its first one on, `entry` is the page table's entry for it; a step
+    // is S::kTile keys on.  Its place inside a page is the same in every step (a tile is whole pages).
+    constexpr int kPagesPerTile = S::kTile / kPage;
+    const int in_page = warp * S::kKeys % kPage;
+    int rem = len - (tile * S::kTile + warp * S::kKeys);
+    const int32_t* entry = p.page_table + (size_t)r * p.max_pages_per_req + tile * kPagesPerTile + warp * S::kKeys / kPage;
+    const int last_rem = len - ((tile_end - 1) * S::kTile + warp * S::kKeys);       // (of the segment's last step)
+    const size_t page_bytes = (size_t)p.n_kv_heads * kPage * S::kRow;
+    const size_t in_head = ((size_t)h * kPage + in_page) * S::kRow;
+    // the page of a step that is `ahead` steps on: only read where that step has keys
+    auto page_ahead = [&](int ahead) { return rem - ahead * S::kTile >= last_rem && rem - ahead * S::kTile > 0 ? __ldcg(entry + ahead * kPagesPerTile) : 0; };
+    int page0 = page_ahead(0), page1 = page_ahead(1);
+    uint4 kr[8], vr[8];
+    // (n keys of the step are stored; what lies behind them is not read)
+    auto load_k = [&](size_t off, int n) {
+      const char* b = p.k_pool + off + c * S::kRow + t * 16;
+#pragma unroll
+      for (int s = 0; s < 2 * S::kSub; ++s)
+#pragma unroll
+        for (int u = 0; u < S::kU; ++u)
+          kr[s * S::kU + u] = n >= S::kKeys || s * 8 + c < n ? ld16(b + s * 8 * S::kRow + u * 64) : make_uint4(0, 0, 0, 0);
+    };
+    auto load_v = [&](size_t off, int n) {
+      const char* b = p.v_pool + off + 2 * t * S::kRow + c * 16;
+#pragma unroll
+      for (int s = 0; s < 4 * S::kSub; ++s)
+#pragma unroll
+        for (int u = 0; u < S::kV; ++u) {
+          const int key = (s >> 2) * 16 + (s & 1) + ((s >> 1) & 1) * 8;      // (+ 2t: this lane's)
+          vr[s * S::kV + u] = n >= S::kKeys || key + 2 * t < n ? ld16(b + key * S::kRow + u * 128) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    auto inside = [&](int page) { return (unsigned)page < (unsigned)p.num_pages; };
+    // (the stream starts before the queries are looked at)
+    bool work = rem > 0 && inside(page0);
+    if (work) { load_k(page0 * page_bytes + in_head, rem); load_v(page0 * page_bytes + in_head, rem); }
     // queries: head c of each block, in the order in which the lanes hold a key's row
     uint32_t qf[NB][16 * S::kRow / 256 * (F8 ? 2 : 1)];
     float fac[NB][2];
@@ -184,7 +238,7 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const int g = hb * HB + nb * 8 + c;
-        const __nv_bfloat16* q = p.q + (((size_t)r * p.n_kv_heads + h) * p.group + g) * D;
+        const bf16* q = p.q + (((size_t)r * p.n_kv_heads + h) * p.group + g) * D;
         constexpr int kQ = D / 32;             // 16-byte pieces of q a lane holds
         uint4 v[kQ];
 #pragma unroll
@@ -236,43 +290,14 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
       }
     }
 
-    uint4 kr[8], vr[8];
-    // keys of this warp's step of a tile that are stored, and the page entry that holds them
-    auto step_keys = [&](int tl) { return max(0, min(S::kKeys, len - (tl * S::kTile + warp * S::kKeys))); };
-    auto page_at = [&](int tl) { return tl < tile_end && step_keys(tl) > 0 ? pages[(tl * S::kTile + warp * S::kKeys) / kPage] : 0; };
-    auto offset = [&](int page, int tl) {
-      return (((size_t)page * p.n_kv_heads + h) * kPage + (tl * S::kTile + warp * S::kKeys) % kPage) * S::kRow;
-    };
-    auto load_k = [&](size_t off, int n) {
-      const char* b = p.k_pool + off + c * S::kRow + t * 16;
-#pragma unroll
-      for (int s = 0; s < 2 * S::kSub; ++s)
-#pragma unroll
-        for (int u = 0; u < S::kU; ++u)
-          kr[s * S::kU + u] = n == S::kKeys || s * 8 + c < n ? ld16(b + s * 8 * S::kRow + u * 64) : make_uint4(0, 0, 0, 0);
-    };
-    auto load_v = [&](size_t off, int n) {
-      const char* b = p.v_pool + off + 2 * t * S::kRow + c * 16;
-#pragma unroll
-      for (int s = 0; s < 4 * S::kSub; ++s)
-#pragma unroll
-        for (int u = 0; u < S::kV; ++u) {
-          const int key = (s >> 2) * 16 + (s & 1) + ((s >> 1) & 1) * 8;      // (+ 2t: this lane's)
-          vr[s * S::kV + u] = n == S::kKeys || key + 2 * t < n ? ld16(b + key * S::kRow + u * 128) : make_uint4(0, 0, 0, 0);
-        }
-    };
-    int n0 = step_keys(tile), pg = page_at(tile), pg_next = page_at(tile + 1);
-    bool bad = n0 > 0 && (pg < 0 || pg >= p.num_pages);
-    size_t off = offset(pg, tile);
-    if (n0 > 0 && !bad) { load_k(off, n0); load_v(off, n0); }
+    [[maybe_unused]] float* score = nullptr;     // of this warp's first key of the step
+    if constexpr (W)
+      score = p.scores + (((size_t)r * p.n_kv_heads + h) * p.max_pages_per_req * kPage + tile * S::kTile + warp * S::kKeys) * p.group + hb * HB;
 
     for (; tile < tile_end; ++tile) {
-      const bool more = tile + 1 < tile_end;
-      const int n1 = more ? step_keys(tile + 1) : 0;
-      const bool bad1 = n1 > 0 && (pg_next < 0 || pg_next >= p.num_pages);
-      const size_t off1 = offset(pg_next, tile + 1);
-      pg_next = page_at(tile + 2);
-      const bool work = n0 > 0 && !bad, work1 = n1 > 0 && !bad1;
+      const bool more = tile + 1 < tile_end, work1 = more && rem > S::kTile && inside(page1);
+      const size_t off1 = page1 * page_bytes + in_head;
+      const int page2 = page_ahead(2);
       float s[NB][S::kSub][4];
       if (work) {
 #pragma unroll
@@ -289,8 +314,9 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
             if constexpr (F8) {
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const uint32_t wl = word(lo, i), wh = word(hi, i);
-                const uint32_t a[4] = {e4m3x2_to_f16x2(wl), e4m3x2_to_f16x2(wh), e4m3x2_to_f16x2(wl >> 16), e4m3x2_to_f16x2(wh >> 16)};
+                uint32_t a[4];
+                e4m3x4_to_f16(word(lo, i), a[0], a[2]);
+                e4m3x4_to_f16(word(hi, i), a[1], a[3]);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) mma16816<F8>(s[nb][b], a, qf[nb][(u * 4 + i) * 2], qf[nb][(u * 4 + i) * 2 + 1]);
               }
@@ -304,58 +330,58 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
             }
           }
       }
-      if (work1) load_k(off1, n1);
-      if constexpr (W) {
-        if (bad) {                               // (the weights kernel reads every stored position)
-          const int j0 = tile * S::kTile + warp * S::kKeys;
-          float* to = p.scores + (((size_t)r * p.n_kv_heads + h) * p.max_pages_per_req * kPage + j0) * p.group;
-          for (int i = lane; i < n0 * HB; i += 32)
-            if (hb * HB + i % HB < p.group) to[(size_t)(i / HB) * p.group + hb * HB + i % HB] = -INFINITY;
-        }
+      if (work1) load_k(off1, rem - S::kTile);
+      if (rem > 0 && !work) {                    // a page outside the pool: its keys are left out
+        if (lane == 0) atomicOr(p.status, FB_ST_BAD_PAGE);
+        if constexpr (W)                         // (the scores of every stored position are read again)
+          for (int i = lane; i < min(rem, S::kKeys) * HB; i += 32)
+            if (hb * HB + i % HB < p.group) score[(size_t)(i / HB) * p.group + i % HB] = -INFINITY;
       }
-      if (bad && lane == 0) atomicOr(p.status, FB_ST_BAD_PAGE);
       if (work) {
         bool move = false;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int b = 0; b < S::kSub; ++b)
+          for (int j = 0; j < 2; ++j) {
+            // rows c and c + 8 of each block of keys, head 2t + j
+            float top = kNoRef;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              // rows c (k < 2) and c + 8 of the block, heads 2t and 2t + 1
-              float x = s[nb][b][k] * fac[nb][k & 1];
-              if (n0 < S::kKeys && b * 16 + (k >> 1) * 8 + c >= n0) x = -INFINITY;
-              s[nb][b][k] = x;
-              move |= x > ref[nb][k & 1] + kRebase;
+            for (int b = 0; b < S::kSub; ++b) {
+              s[nb][b][j] *= fac[nb][j];
+              s[nb][b][j + 2] *= fac[nb][j];
+              if (rem < S::kKeys) {
+                if (b * 16 + c >= rem) s[nb][b][j] = -INFINITY;
+                if (b * 16 + 8 + c >= rem) s[nb][b][j + 2] = -INFINITY;
+              }
+              top = fmaxf(top, fmaxf(s[nb][b][j], s[nb][b][j + 2]));
             }
+            move |= top > ref[nb][j] + (kRebase + kShift);
+          }
         if constexpr (W) {
-          const int j0 = tile * S::kTile + warp * S::kKeys;
-          float* to = p.scores + (((size_t)r * p.n_kv_heads + h) * p.max_pages_per_req * kPage + j0) * p.group;
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            const int g = hb * HB + nb * 8 + 2 * t;
+          for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int b = 0; b < S::kSub; ++b)
 #pragma unroll
               for (int k = 0; k < 4; k += 2) {
-                const int j = b * 16 + (k >> 1) * 8 + c;
-                if (j >= n0) continue;
-                float* w = to + (size_t)j * p.group + g;
-                if (g + 1 < p.group) *reinterpret_cast<float2*>(w) = make_float2(s[nb][b][k], s[nb][b][k + 1]);
-                else if (g < p.group) *w = s[nb][b][k];
+                const int j = b * 16 + (k >> 1) * 8 + c, g = nb * 8 + 2 * t;
+                if (j >= rem) continue;
+                float* w = score + j * p.group + g;
+                if (hb * HB + g + 1 < p.group) *reinterpret_cast<float2*>(w) = make_float2(s[nb][b][k], s[nb][b][k + 1]);
+                else if (hb * HB + g < p.group) *w = s[nb][b][k];
               }
-          }
         }
         if (__any_sync(0xffffffffu, move)) {     // rare after the first steps: the reference goes up to the largest score
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              float m = ref[nb][j];
+              float m = ref[nb][j] + kShift;
 #pragma unroll
               for (int b = 0; b < S::kSub; ++b) m = fmaxf(m, fmaxf(s[nb][b][j], s[nb][b][j + 2]));
 #pragma unroll
               for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+              m -= kShift;
               const float f = ex2(ref[nb][j] - m);
               ref[nb][j] = m;
               sum[nb][j] *= f;
@@ -370,7 +396,7 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
           for (int b = 0; b < S::kSub; ++b)
 #pragma unroll
             for (int k = 0; k < 4; k += 2) {
-              const float p0 = ex2(s[nb][b][k] - ref[nb][0] + kShift), p1 = ex2(s[nb][b][k + 1] - ref[nb][1] + kShift);
+              const float p0 = ex2(s[nb][b][k] - ref[nb][0]), p1 = ex2(s[nb][b][k + 1] - ref[nb][1]);
               sum[nb][0] += p0;                  // (the sums are of the weights before they are rounded)
               sum[nb][1] += p1;
               uint32_t two;
@@ -388,9 +414,7 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
                 const uint32_t w0 = word(vr[b * 4 + 2 * k], i >> 1), w1 = word(vr[b * 4 + 2 * k + 1], i >> 1);
-                const uint32_t z = __byte_perm(w0, w1, i & 1 ? 0x7362 : 0x5140);
-                a[2 * k] = e4m3x2_to_f16x2(z);
-                a[2 * k + 1] = e4m3x2_to_f16x2(z >> 16);
+                e4m3x4_to_f16(__byte_perm(w0, w1, i & 1 ? 0x7362 : 0x5140), a[2 * k], a[2 * k + 1]);
               }
             } else if constexpr (D == 128) {
 #pragma unroll
@@ -411,8 +435,12 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
             for (int nb = 0; nb < NB; ++nb) mma16816<F8>(o[nb][i], a, pt[nb][b][0], pt[nb][b][1]);
           }
       }
-      if (work1) load_v(off1, n1);
-      n0 = n1; bad = bad1; off = off1;
+      if (work1) load_v(off1, rem - S::kTile);
+      work = work1;
+      page1 = page2;
+      rem -= S::kTile;
+      entry += kPagesPerTile;
+      if constexpr (W) score += S::kTile * p.group;
     }
 
     // the four warps' shares of the segment, added in order
@@ -434,12 +462,13 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
         }
       }
     __syncthreads();
-    const bool begins = tile_end == seg, ends = tile_end == nt, whole = begins && ends;
+    const bool begins = tile_end == seg, whole = begins && tile_end == nt;
     const int slot = 2 * (int)blockIdx.x + (begins ? 1 : 0);
     const float vs = F8 ? p.v_scale[h] : 1.f;
-    for (int i = tid; i < HB * D; i += kTokThreads) {
+    bf16* out = p.out + (((size_t)r * p.n_kv_heads + h) * p.group + hb * HB) * D;
+    const int heads = min(HB, p.group - hb * HB);
+    for (int i = tid; i < heads * D; i += kTokThreads) {
       const int g = i / D, d = i % D;
-      if (hb * HB + g >= p.group) break;
       float m = sh_ml[0][g].x;
 #pragma unroll
       for (int w = 1; w < kTokWarps; ++w) m = fmaxf(m, sh_ml[w][g].x);
@@ -451,141 +480,164 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
         x += sh_o[w][g * kStride + d] * f;
       }
       if (whole) {
-        p.out[(((size_t)r * p.n_kv_heads + h) * p.group + hb * HB + g) * D + d] = __float2bfloat16_rn(l == 0.f ? 0.f : x / l * vs);
-        if constexpr (W)
-          if (d == 0) p.row_ml[((size_t)r * rows + row) * HB + g] = make_float2(m, l);
+        out[i] = __float2bfloat16_rn(l == 0.f ? 0.f : x / l * vs);
+        if (W && d == 0) p.row_ml[((size_t)r * rows + row) * HB + g] = make_float2(m, l);
       } else {
-        p.part_o[((size_t)slot * HB + g) * D + d] = x;
+        p.part_o[(size_t)slot * HB * D + i] = x;
         if (d == 0) p.part_ml[(size_t)slot * HB + g] = make_float2(m, l);
       }
     }
     left -= seg;
     if (left <= 0) break;
-    __syncthreads();
+    __syncthreads();                             // (sh_o is read no more)
     tile = 0;                                    // (the segment ended with its row: the next row starts)
     if (++row == rows) {
       row = 0;
-      do { ++r; nt = tok_tiles(p, r, S::kTile); } while (nt == 0 && r < p.requests);
+      do { ++r; len = tok_len(p, r); nt = tok_tiles(p, len, S::kTile); } while (nt == 0 && r < p.requests);
       if (nt == 0) break;
     }
   }
 }
 
 // ---------------------------------------------------------------- the join
-// The pieces of a row: CTAs c0..c1 of the deal; piece i lies in slot 2 i + 1 where the row starts in that CTA.
-struct TokPieces { long long start, share; int c0, n; };
-__device__ __forceinline__ TokPieces tok_pieces(long long start, int nt, long long share) {
-  TokPieces k;
-  k.start = start; k.share = share;
-  k.c0 = (int)(start / share);
-  k.n = (int)((start + nt - 1) / share) - k.c0 + 1;
-  return k;
+// kv_weight[r, h, j] += sum over the group of exp(score - reference) / sum, from the scores that the stream has left, for
+// the positions of a slice, a position to a thread.  16 bytes of scores a key for a group of four, written and read,
+// against 256 to 512 of K and V: cheaper than forming them again.
+constexpr int kWeightAt = 4;                     // positions of a thread at once
+__device__ __forceinline__ void add_weights(const TokenParams& p, const float2* top, size_t base, int len, int slice, int slices) {
+  constexpr int kStep = kWeightAt * kTokThreads;
+  for (long long j0 = (long long)slice * kStep + threadIdx.x; j0 < len; j0 += (long long)slices * kStep) {
+    float w[kWeightAt], old[kWeightAt];
+#pragma unroll
+    for (int u = 0; u < kWeightAt; ++u) {
+      w[u] = 0.f;
+      old[u] = j0 + u * kTokThreads < len ? __ldcg(p.kv_weight + base + j0 + u * kTokThreads) : 0.f;
+    }
+    if (p.group % 4 == 0) {
+      for (int g = 0; g < p.group; g += 4) {
+        float4 v[kWeightAt];
+#pragma unroll
+        for (int u = 0; u < kWeightAt; ++u)
+          v[u] = j0 + u * kTokThreads < len ? __ldcg(reinterpret_cast<const float4*>(p.scores + (base + j0 + u * kTokThreads) * p.group + g))
+                                            : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float2 a = top[g], b = top[g + 1], x = top[g + 2], y = top[g + 3];
+#pragma unroll
+        for (int u = 0; u < kWeightAt; ++u) {
+          w[u] += ex2(v[u].x - a.x) * a.y; w[u] += ex2(v[u].y - b.x) * b.y;
+          w[u] += ex2(v[u].z - x.x) * x.y; w[u] += ex2(v[u].w - y.x) * y.y;
+        }
+      }
+    } else {
+      for (int g = 0; g < p.group; ++g)
+#pragma unroll
+        for (int u = 0; u < kWeightAt; ++u)
+          if (j0 + u * kTokThreads < len) w[u] += ex2(__ldcg(p.scores + (base + j0 + u * kTokThreads) * p.group + g) - top[g].x) * top[g].y;
+    }
+#pragma unroll
+    for (int u = 0; u < kWeightAt; ++u)
+      if (j0 + u * kTokThreads < len) p.kv_weight[base + j0 + u * kTokThreads] = old[u] + w[u];
+  }
 }
-__device__ __forceinline__ int tok_slot(const TokPieces& k, int i) { return 2 * (k.c0 + i) + ((k.c0 + i) * k.share <= k.start ? 1 : 0); }
 
-// blockIdx.y < heads of a block: joins the pieces of one query head of row blockIdx.x, in order, a piece to D / 4 threads.
-// Beyond (weights): adds the softmax weights of a slice of the positions of a (request, KV head).
+// blockIdx.y < p.join_ctas: joins the pieces of every join_ctas-th query head of row blockIdx.x, in order, a piece to D / 4
+// threads.  Beyond (weights): a slice of the positions of a (request, KV head).
 template <int D, bool F8, int NB, bool W>
 __global__ void __launch_bounds__(kTokThreads) token_join_kernel(const TokenParams p) {
   using S = TokShape<D, F8>;
-  constexpr int HB = 8 * NB;
-  __shared__ float fac[2 * kTokCtasPerSm * kSms];
-  __shared__ float red[kTokThreads * 4];
-  __shared__ float2 top[kTileM];                 // (a group has at most 128 heads)
+  constexpr int HB = 8 * NB, kLanes = D / 4, kGroups = kTokThreads / kLanes, kAhead = 8;
+  __shared__ float2 ml[kMostPieces + 2];
+  __shared__ float4 red[kTokThreads];
+  __shared__ float sums[kTokWarps], tops[kTokWarps];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rows = p.n_kv_heads * p.head_blocks;
-  const bool weights = W && (int)blockIdx.y >= HB;
+  const bool weights = W && (int)blockIdx.y >= p.join_ctas;
   const int r = blockIdx.x / rows, row = blockIdx.x % rows, h = row / p.head_blocks, hb = row % p.head_blocks;
-  if (weights && hb != 0) return;
-  if (!weights && hb * HB + (int)blockIdx.y >= p.group) return;
+  // (the kernel behind this one waits for this one alone: one CTA at least has to have waited for the stream)
+  const bool keeper = blockIdx.x == 0 && blockIdx.y == 0;
   // (the lengths are older than the stream kernel, which waited itself before it let this one start)
-  const int nt = tok_tiles(p, r, S::kTile);
-  if (nt == 0) return;
-  long long before;
-  const long long share = tok_share(tok_total(p, S::kTile, r, before), p.n_ctas);
-  const TokPieces k = tok_pieces(before + (long long)row * nt, nt, share);
+  const int first = tok_len(p, lane), len = tok_len(p, r), nt = tok_tiles(p, len, S::kTile);
+  const bool idle = nt == 0 || (weights && hb != 0);
+  if (idle && !keeper) return;
+  const TokDeal deal = tok_deal(p, S::kTile, first, r);
+  const TokPieces k(deal.before + (long long)row * nt, nt, deal.share);
+  if (keeper || weights || k.n > 1) pdl_wait_only();
+  if (idle) return;
   if (!weights) {
     if (k.n == 1) return;
-    pdl_wait_only();
-    const int g = blockIdx.y;
+    for (int g = blockIdx.y; g < min(HB, p.group - hb * HB); g += p.join_ctas) {
+    const int grp = tid / kLanes, d4 = tid % kLanes;
+    const float vs = F8 ? p.v_scale[h] : 1.f;
+    // the outputs of the first pieces are under way while references and sums are put together
+    auto piece = [&](int i) { return __ldcg(reinterpret_cast<const float4*>(p.part_o + ((size_t)k.slot(i) * HB + g) * D) + d4); };
+    float4 v[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) v[u] = grp + u * kGroups < k.n ? piece(grp + u * kGroups) : make_float4(0.f, 0.f, 0.f, 0.f);
     float m = kNoRef;
     for (int i = tid; i < k.n; i += kTokThreads) {
-      const float2 v = p.part_ml[(size_t)tok_slot(k, i) * HB + g];
-      fac[2 * i] = v.x; fac[2 * i + 1] = v.y;
-      m = fmaxf(m, v.x);
+      const float2 x = __ldcg(p.part_ml + (size_t)k.slot(i) * HB + g);
+      ml[i] = x;
+      m = fmaxf(m, x.x);
     }
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-    if (lane == 0) red[warp] = m;
+    if (lane == 0) tops[warp] = m;
     __syncthreads();
-    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    constexpr int kLanes = D / 4, kGroups = kTokThreads / kLanes;
-    const int grp = tid / kLanes, d4 = tid % kLanes;
+    m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-#pragma unroll 4
-    for (int i = grp; i < k.n; i += kGroups) {
-      const float f = ex2(fac[2 * i] - m);
-      const float4 v = reinterpret_cast<const float4*>(p.part_o + ((size_t)tok_slot(k, i) * HB + g) * D)[d4];
-      acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
-      l += fac[2 * i + 1] * f;
+    for (int i0 = grp; i0 < k.n; i0 += kAhead * kGroups) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int i = i0 + u * kGroups, next = i + kAhead * kGroups;
+        if (i < k.n) {
+          const float f = ex2(ml[i].x - m);
+          acc.x += v[u].x * f; acc.y += v[u].y * f; acc.z += v[u].z * f; acc.w += v[u].w * f;
+        }
+        if (next < k.n) v[u] = piece(next);
+      }
     }
-    __syncthreads();
-    reinterpret_cast<float4*>(red)[tid] = acc;
-    __shared__ float suml[kGroups];
-    if (d4 == 0) suml[grp] = l;
+    float l = 0.f;
+    for (int i = tid; i < k.n; i += kTokThreads) l += ml[i].y * ex2(ml[i].x - m);
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+    if (lane == 0) sums[warp] = l;
+    red[tid] = acc;
     __syncthreads();
     if (tid < D) {
-      float x = 0.f, s = 0.f;
+      float x = 0.f;
 #pragma unroll
-      for (int w = 0; w < kGroups; ++w) { x += red[w * D + tid]; s += suml[w]; }
-      const float vs = F8 ? p.v_scale[h] : 1.f;
+      for (int w = 0; w < kGroups; ++w) x += reinterpret_cast<const float*>(red)[w * D + tid];
+      const float s = (sums[0] + sums[1]) + (sums[2] + sums[3]);
       p.out[(((size_t)r * p.n_kv_heads + h) * p.group + hb * HB + g) * D + tid] = __float2bfloat16_rn(s == 0.f ? 0.f : x / s * vs);
     }
+    __syncthreads();
+    }
   } else if constexpr (W) {
-    pdl_wait_only();
-    constexpr float kShift = F8 ? 7.f : 0.f;
-    // reference and sum of every query head, over the pieces of its row
+    __shared__ float2 top[kTileM];               // reference, 1 / sum (a group has at most 128 heads)
     for (int g = warp; g < p.group; g += kTokWarps) {
       const int b = g / HB, gl = g % HB;
-      const TokPieces q = tok_pieces(before + (long long)(row + b) * nt, nt, share);
+      const TokPieces q(deal.before + (long long)(row + b) * nt, nt, deal.share);
       float m = kNoRef, l = 0.f;
       if (q.n == 1) {
-        const float2 v = p.row_ml[((size_t)r * rows + row + b) * HB + gl];
+        const float2 v = __ldcg(p.row_ml + ((size_t)r * rows + row + b) * HB + gl);
         m = v.x; l = v.y;
       } else {
-        for (int i = lane; i < q.n; i += 32) m = fmaxf(m, p.part_ml[(size_t)tok_slot(q, i) * HB + gl].x);
+        for (int i0 = 0; i0 < q.n; i0 += 32) {   // running reference and sum, 32 pieces at a time
+          const float2 v = i0 + lane < q.n ? __ldcg(p.part_ml + (size_t)q.slot(i0 + lane) * HB + gl) : make_float2(kNoRef, 0.f);
+          float mx = fmaxf(m, v.x);
 #pragma unroll
-        for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-        for (int i = lane; i < q.n; i += 32) {
-          const float2 v = p.part_ml[(size_t)tok_slot(q, i) * HB + gl];
-          l += v.y * ex2(v.x - m);
+          for (int x = 16; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+          float add = v.y * ex2(v.x - mx);
+#pragma unroll
+          for (int x = 16; x > 0; x >>= 1) add += __shfl_xor_sync(0xffffffffu, add, x);
+          l = l * ex2(m - mx) + add;
+          m = mx;
         }
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
       }
-      if (lane == 0) top[g] = make_float2(m - kShift, l == 0.f ? 0.f : 1.f / l);
+      if (lane == 0) top[g] = make_float2(m, l == 0.f ? 0.f : 1.f / l);
     }
     __syncthreads();
-    const int len = __ldcg(p.kv_len + r), slices = gridDim.y - HB;
-    const size_t base = ((size_t)r * p.n_kv_heads + h) * p.max_pages_per_req * kPage;
-    for (int j = ((int)blockIdx.y - HB) * kTokThreads + tid; j < len; j += slices * kTokThreads) {
-      const float* s = p.scores + (base + j) * p.group;
-      float w = 0.f;
-      if (p.group % 4 == 0) {
-        for (int g = 0; g < p.group; g += 4) {
-          const float4 v = *reinterpret_cast<const float4*>(s + g);
-          w += ex2(v.x - top[g].x) * top[g].y;
-          w += ex2(v.y - top[g + 1].x) * top[g + 1].y;
-          w += ex2(v.z - top[g + 2].x) * top[g + 2].y;
-          w += ex2(v.w - top[g + 3].x) * top[g + 3].y;
-        }
-      } else {
-        for (int g = 0; g < p.group; ++g) w += ex2(s[g] - top[g].x) * top[g].y;
-      }
-      p.kv_weight[base + j] += w;
-    }
+    add_weights(p, top, ((size_t)r * p.n_kv_heads + h) * p.max_pages_per_req * kPage, len, blockIdx.y - p.join_ctas, gridDim.y - p.join_ctas);
   }
 }
 
@@ -615,11 +667,11 @@ static int launch_token(fb_ctx* ctx, const TokenParams& p, cudaStream_t stream) 
   const fb_config& c = ctx->cfg;
   if (int e = cuda_err(ctx, launch_pdl(token_attn_kernel<D, F8, NB, W>, p.n_ctas, kTokThreads, 0, stream, p), "token_attn_kernel launch"))
     return e;
-  const long long rows = (long long)c.max_requests * c.n_kv_heads * p.head_blocks, pairs = (long long)c.max_requests * c.n_kv_heads;
-  const long long blocks = ((long long)c.max_pages_per_req * kPage + kTokThreads - 1) / kTokThreads;
-  const long long want = 1 + 8 * kSms / pairs;
+  const long long pairs = (long long)c.max_requests * c.n_kv_heads, step = kWeightAt * kTokThreads;
+  const long long blocks = ((long long)c.max_pages_per_req * kPage + step - 1) / step, want = 1 + 12 * kSms / pairs;
   const int slices = W ? (int)(want < blocks ? want : blocks) : 0;
-  return cuda_err(ctx, launch_pdl(token_join_kernel<D, F8, NB, W>, dim3((unsigned)rows, 8 * NB + slices), kTokThreads, 0, stream, p),
+  // (a CTA a head where rows are few, one for all heads of a row where they fill the machine)
+  return cuda_err(ctx, launch_pdl(token_join_kernel<D, F8, NB, W>, dim3((unsigned)(pairs * p.head_blocks), p.join_ctas + slices), kTokThreads, 0, stream, p),
                   "token_join_kernel launch");
 }
 template <int D, bool F8>
@@ -639,9 +691,9 @@ int launch_token_attn(fb_ctx* ctx, const fb_cache* kv, const void* q, const void
     return set_err(ctx, FB_ERR_UNSUPPORTED, "max_requests * n_q_heads must be below 2^31");
   TokenParams p;
   p.kv_len = kv->kv_len; p.page_table = kv->page_table; p.kv_weight = kv->kv_weight;
-  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.q = static_cast<const bf16*>(q);
   p.k_pool = static_cast<const char*>(k_pool); p.v_pool = static_cast<const char*>(v_pool);
-  p.k_scale = k_scale; p.v_scale = v_scale; p.out = static_cast<__nv_bfloat16*>(out); p.status = status;
+  p.k_scale = k_scale; p.v_scale = v_scale; p.out = static_cast<bf16*>(out); p.status = status;
   p.part_ml = reinterpret_cast<float2*>(base + w.part_ml);
   p.part_o = reinterpret_cast<float*>(base + w.part_o);
   p.row_ml = reinterpret_cast<float2*>(base + w.row_ml);
@@ -649,6 +701,9 @@ int launch_token_attn(fb_ctx* ctx, const fb_cache* kv, const void* q, const void
   p.requests = c.max_requests; p.group = ctx->group; p.n_kv_heads = c.n_kv_heads;
   p.head_blocks = (ctx->group + hb - 1) / hb;
   p.max_pages_per_req = c.max_pages_per_req; p.num_pages = c.num_pages; p.n_ctas = tok_ctas(ctx);
+  const long long rows = (long long)c.max_requests * c.n_kv_heads * p.head_blocks, per_row = 8 * kSms / rows;
+  const int heads = ctx->group < hb ? ctx->group : hb;
+  p.join_ctas = per_row < 1 ? 1 : per_row < heads ? (int)per_row : heads;
   p.sm_scale = ctx->sm_scale;
   if (c.kv_fp8) return launch_token<128, true>(ctx, p, accumulate, stream);
   return c.head_dim == 128 ? launch_token<128, false>(ctx, p, accumulate, stream)
