@@ -489,6 +489,32 @@ int fb_token_attn_fp8(fb_ctx* ctx, const fb_cache* cache, const void* q,
                       int32_t accumulate, void* ws, int32_t* status,
                       void* stream);
 
+/* Cuts every cache that holds more than keep[r] keys to keep[r] of them, for each
+ * KV head by itself.  The keys that stay are the first keep[r] in this order:
+ * protected ones (kv_pos < sinks, or among the last `recent` positions, kv_pos >
+ * tok_pos - recent) by storage position, then the others by greater kv_weight and
+ * then by lower storage position; a NaN weight ranks below every number.  With m = keep[r]: the
+ * i-th storage position below m that becomes free takes over what the i-th
+ * position at or above m that stays holds, K and V rows, kv_pos and kv_weight;
+ * nothing else moves, and kv_len becomes m.  (Attention does not see the order in
+ * which keys are stored.)  Requests with keep[r] < 0 or kv_len <= keep[r] stay as
+ * they are; pages behind the new kv_len are the caller's again.
+ *   keep          [R_max] int32, DEVICE pointer
+ *   recent, sinks at least 0
+ *   k_pool,v_pool the pools of the context, bf16 or 8-bit (rows are moved as they
+ *                 are); pages that requests share must not be evicted from
+ *   ws            fb_evict_workspace_bytes(ctx) bytes of device scratch, 256-byte
+ *                 aligned; nothing in it outlives the call
+ * A request with a page outside the pool below kv_len is left as it is and
+ * FB_ST_BAD_PAGE set.  After an eviction storage positions are not absolute
+ * positions any more: a caller that goes on with the block decoder on such a
+ * request (prefix_len = kv_len) rotates its queries and keys itself, by its own
+ * count of positions, and leaves rope_base at 0. */
+size_t fb_evict_workspace_bytes(const fb_ctx* ctx);
+int fb_evict_kv(fb_ctx* ctx, const fb_cache* cache, const int32_t* keep,
+                int32_t recent, int32_t sinks, void* k_pool, void* v_pool,
+                void* ws, int32_t* status, void* stream);
+
 /* One whole step (the four calls above in order) on HOST inputs: copies this
  * step's q / k_win / v_win / logits from host (pinned) memory into the
  * caller's device staging buffers, runs the step, and copies n_committed,

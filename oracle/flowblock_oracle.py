@@ -903,9 +903,9 @@ def add_weights(cfg: Config, kv_len, kv_weight, weights):
 def evict_kv(cfg: Config, kv_len, tok_pos, kv_pos, kv_weight, page_table, keep, recent: int, sinks: int, k_pool, v_pool):
     """Cuts every cache of more than keep[r] keys to that many, per KV head.
     The keys that stay are the first keep[r] in the order: protected ones
-    (position below ``sinks`` or among the last ``recent`` positions) before the
-    others, then greater weight, then lower storage index; a NaN weight ranks
-    below every number.  With n' = keep[r]: the i-th storage index below n' that
+    (position below ``sinks`` or among the last ``recent`` positions) by storage
+    index, then the others by greater weight, then by lower storage index; a NaN
+    weight ranks below every number.  With n' = keep[r]: the i-th storage index below n' that
     goes takes over what the i-th index at or above n' that stays holds.  In
     place; keep[r] < 0: the request is left alone."""
     ps = cfg.page_size
@@ -917,9 +917,10 @@ def evict_kv(cfg: Config, kv_len, tok_pos, kv_pos, kv_weight, page_table, keep, 
             def rank(j):
                 p, w = int(kv_pos[r, h, j]), float(kv_weight[r, h, j])
                 safe = p < sinks or p > int(tok_pos[r]) - recent
-                return (not safe, np.isnan(w), 0.0 if np.isnan(w) else -w, j)
+                return (not safe, not safe and np.isnan(w), 0.0 if safe or np.isnan(w) else -w, j)
             stays = sorted(sorted(range(n), key=rank)[:m])
-            holes = [j for j in range(m) if j not in set(stays)]
+            kept = set(stays)
+            holes = [j for j in range(m) if j not in kept]
             above = [j for j in stays if j >= m]
             for to, at in zip(holes, above):
                 pt, pa = int(page_table[r, to // ps]), int(page_table[r, at // ps])

@@ -34,7 +34,7 @@ EXPORTS = ["fb_create", "fb_destroy", "fb_last_error", "fb_workspace_bytes",
            "fb_lm_head_workspace_bytes", "fb_set_tuning", "fb_attn_plan_host",
            "fb_scatter_window_kv_fp8", "fb_wavefront_attn_fp8", "fb_append_kv",
            "fb_append_kv_fp8", "fb_token_workspace_bytes", "fb_token_attn",
-           "fb_token_attn_fp8"]
+           "fb_token_attn_fp8", "fb_evict_workspace_bytes", "fb_evict_kv"]
 
 
 class fb_config(C.Structure):
@@ -88,7 +88,8 @@ class fb_device_bufs(C.Structure):
 # the calls that _marshal makes, in the order of its bind()
 _FAST = ("fb_pack_wavefronts", "fb_wavefront_attn", "fb_t2t_step", "fb_gate_commit", "fb_scatter_window_kv",
          "fb_scatter_window_kv_fp8", "fb_wavefront_attn_fp8", "fb_embed_gather", "fb_lm_head_t2t",
-         "fb_wavefront_attn_static", "fb_append_kv", "fb_append_kv_fp8", "fb_token_attn", "fb_token_attn_fp8")
+         "fb_wavefront_attn_static", "fb_append_kv", "fb_append_kv_fp8", "fb_token_attn", "fb_token_attn_fp8",
+         "fb_evict_kv")
 
 _lib = None
 _m = None
@@ -139,12 +140,16 @@ def lib() -> C.CDLL:
         l.fb_token_workspace_bytes.restype = C.c_size_t
         l.fb_token_attn.argtypes = [P, C.POINTER(fb_cache)] + [P] * 4 + [C.c_int32, P, P, P]
         l.fb_token_attn_fp8.argtypes = [P, C.POINTER(fb_cache)] + [P] * 6 + [C.c_int32, P, P, P]
+        l.fb_evict_workspace_bytes.argtypes = [P]
+        l.fb_evict_workspace_bytes.restype = C.c_size_t
+        l.fb_evict_kv.argtypes = [P, C.POINTER(fb_cache), P, C.c_int32, C.c_int32] + [P] * 5
         l.fb_step_host.argtypes = [P, C.POINTER(fb_state), C.POINTER(fb_pack),
                                    C.POINTER(fb_device_bufs),
                                    C.POINTER(fb_host_io), P]
         for n in EXPORTS:
             if n not in ("fb_last_error", "fb_workspace_bytes",
-                         "fb_lm_head_workspace_bytes", "fb_token_workspace_bytes"):
+                         "fb_lm_head_workspace_bytes", "fb_token_workspace_bytes",
+                         "fb_evict_workspace_bytes"):
                 getattr(l, n).restype = I
         try:
             from . import _marshal
@@ -204,7 +209,8 @@ class Context:
         R, H, P = c.max_requests, c.n_kv_heads, c.max_pages_per_req
         self._sizes = (R, R * H * P * c.page_size, R * P, R * H * c.head_dim, R * c.n_q_heads * c.head_dim,
                        c.num_pages * H * c.page_size * c.head_dim, H,
-                       *(lib().fb_token_workspace_bytes(self._h, a) for a in (0, 1)))
+                       *(lib().fb_token_workspace_bytes(self._h, a) for a in (0, 1)),
+                       lib().fb_evict_workspace_bytes(self._h), c.kv_fp8)
         if tuning:
             self.set_tuning(**tuning)
 
@@ -338,6 +344,12 @@ def alloc_token_workspace(ctx: Context, device, accumulate: bool = False) -> tor
     return torch.empty((n + 255) // 256 * 256, dtype=torch.uint8, device=device)
 
 
+def alloc_evict_workspace(ctx: Context, device) -> torch.Tensor:
+    """Scratch of fb_evict_kv."""
+    n = lib().fb_evict_workspace_bytes(ctx.handle)
+    return torch.empty((n + 255) // 256 * 256, dtype=torch.uint8, device=device)
+
+
 # ----------------------------------------------------------------- the calls
 def fb_pack_wavefronts(ctx: Context, st: DeviceState, pk: PackBuffers, ws,
                        status, stream=None):
@@ -453,6 +465,14 @@ def fb_token_attn_fp8(ctx: Context, cache: CacheState, q, k_pool8, v_pool8, k_sc
     """The same over 8-bit (E4M3) pages."""
     rc = _m.token_attn_fp8(ctx._hv, ctx._sizes, _device(), cache, q, k_pool8, v_pool8, out, accumulate, ws, status,
                            _stream(stream), k_scale, v_scale)
+    if rc:
+        ctx.check(rc)
+
+
+def fb_evict_kv(ctx: Context, cache: CacheState, keep, recent: int, sinks: int, k_pool, v_pool, ws, status, stream=None):
+    """Cuts every cache of more than keep[r] keys to that many: the last ``recent`` and the first ``sinks`` positions,
+    then those of greatest accumulated weight.  bf16 or 8-bit pools, as the context says."""
+    rc = _m.evict(ctx._hv, ctx._sizes, _device(), cache, keep, recent, sinks, k_pool, v_pool, ws, status, _stream(stream))
     if rc:
         ctx.check(rc)
 

@@ -19,7 +19,8 @@ LIB = os.path.join(HERE, "libflowblock.so")
 # named for the Python it is built against: another one does not load it
 MARSHAL = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.cu", "pack.cu", "t2t.cu", "gate_commit.cu", "attn_sm100.cu", "scatter.cu", "lm_head.cu",
-           "attn_static.cu", "attn_pair_sm100.cu", "token_attn.cu"]
+           "attn_static.cu", "attn_pair_sm100.cu", "token_attn.cu",
+           "evict.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo",
               "-std=c++17", "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

@@ -443,6 +443,22 @@ int fb_token_attn_fp8(fb_ctx* ctx, const fb_cache* cache, const void* q, const v
   return token_attn(ctx, cache, q, k_pool8, v_pool8, k_scale, v_scale, 1, out, accumulate, ws, status, stream);
 }
 
+size_t fb_evict_workspace_bytes(const fb_ctx* ctx) { return ctx ? fb::evict_workspace_bytes(ctx) : 0; }
+
+int fb_evict_kv(fb_ctx* ctx, const fb_cache* cache, const int32_t* keep, int32_t recent, int32_t sinks, void* k_pool,
+                void* v_pool, void* ws, int32_t* status, void* stream) {
+  if (!ctx) return fail(nullptr, FB_ERR_INVALID_ARG, "ctx is null");
+  if (int e = check_cache(ctx, cache, -1)) return e;
+  if (!cache->tok_pos || !cache->kv_pos || !cache->kv_weight)
+    return fail(ctx, FB_ERR_INVALID_ARG, "cache.tok_pos, cache.kv_pos or cache.kv_weight is null");
+  if (!keep || !k_pool || !v_pool || !status) return fail(ctx, FB_ERR_INVALID_ARG, "a tensor pointer is null");
+  if (recent < 0 || sinks < 0) return fail(ctx, FB_ERR_INVALID_ARG, "recent and sinks must not be negative");
+  if (!ws) return fail(ctx, FB_ERR_WORKSPACE, "workspace is null");
+  if (!aligned16(k_pool) || !aligned16(v_pool)) return fail(ctx, FB_ERR_ALIGNMENT, "tensor pointers must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(ctx, FB_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
+  return fb::launch_evict(ctx, cache, keep, recent, sinks, k_pool, v_pool, ws, status, (cudaStream_t)stream);
+}
+
 int fb_step_host(fb_ctx* ctx, const fb_state* st, const fb_pack* pk, const fb_device_bufs* dev,
                  const fb_host_io* io, void* stream) {
   if (!ctx) return fail(nullptr, FB_ERR_INVALID_ARG, "ctx is null");

@@ -358,6 +358,9 @@ size_t token_workspace_bytes(const fb_ctx*, bool weights);
 int launch_token_attn(fb_ctx*, const fb_cache*, const void* q, const void* k_pool, const void* v_pool,
                       const float* k_scale, const float* v_scale, void* out, int accumulate, void* ws, int32_t* status,
                       cudaStream_t);
+size_t evict_workspace_bytes(const fb_ctx*);
+int launch_evict(fb_ctx*, const fb_cache*, const int32_t* keep, int recent, int sinks, void* k_pool, void* v_pool, void* ws,
+                 int32_t* status, cudaStream_t);
 int launch_t2t(fb_ctx*, const fb_pack*, const void* logits, const fb_state*, int32_t* argmax,
                float* conf, uint8_t* action, int32_t* slot_stats, int32_t* status, cudaStream_t);
 int launch_gate(fb_ctx*, const fb_pack*, const int32_t* slot_stats, const fb_state*,

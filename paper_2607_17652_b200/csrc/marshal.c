@@ -26,7 +26,7 @@ static const char* const k_pack[9] = {"n_live", "slot_req", "slot_s", "slot_pos0
 
 /* entry points, in the order of `names` in bind() */
 enum { F_PACK, F_ATTN, F_T2T, F_GATE, F_SCATTER, F_SCATTER8, F_ATTN8, F_EMBED, F_HEAD, F_STATIC,
-       F_APPEND, F_APPEND8, F_TOKEN, F_TOKEN8, F_COUNT };
+       F_APPEND, F_APPEND8, F_TOKEN, F_TOKEN8, F_EVICT, F_COUNT };
 static void* fn[F_COUNT];
 
 static PyObject* bind(PyObject* self, PyObject* const* args, Py_ssize_t n) {
@@ -202,8 +202,9 @@ static PyObject* m_static(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 }
 
 /* `sizes` of a context, in elements (binding.Context): requests, records, page table, a K or V row a request, a q row a
- * request, a pool, KV heads, bytes of workspace of the attention without and with weights */
-enum { Z_REQ, Z_REC, Z_PT, Z_KV, Z_Q, Z_POOL, Z_HEADS, Z_WS, Z_WS_WEIGHTS, Z_COUNT };
+ * request, a pool, KV heads, bytes of workspace of the attention without and with weights and of the
+ * eviction, whether the pools hold 8 bits */
+enum { Z_REQ, Z_REC, Z_PT, Z_KV, Z_Q, Z_POOL, Z_HEADS, Z_WS, Z_WS_WEIGHTS, Z_WS_EVICT, Z_FP8, Z_COUNT };
 static int as_sizes(PyObject* o, long long* z) {
   if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != Z_COUNT) { PyErr_SetString(PyExc_TypeError, "sizes"); return -1; }
   for (int i = 0; i < Z_COUNT; ++i)
@@ -271,12 +272,26 @@ static PyObject* token(PyObject* self, PyObject* const* a, Py_ssize_t n, int fp8
 static PyObject* m_token(PyObject* self, PyObject* const* a, Py_ssize_t n) { return token(self, a, n, 0); }
 static PyObject* m_token8(PyObject* self, PyObject* const* a, Py_ssize_t n) { return token(self, a, n, 1); }
 
+/* handle, sizes, device, cache, keep, recent, sinks, k_pool, v_pool, ws, status, stream */
+static PyObject* m_evict(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  ARGS(12, "evict") CACHE("fb_evict_kv")
+  int32_t recent, sinks;
+  void* stream;
+  if (as_int(a[5], &recent) || as_int(a[6], &sinks) || as_ptr(a[11], &stream)) return NULL;
+  TENSOR(keep, 4, "fb_evict_kv", "keep", T_I32, z[Z_REQ], 0)
+  TENSOR(kp, 7, "fb_evict_kv", "k_pool", z[Z_FP8] ? T_U8 : T_BF16, z[Z_POOL], 1)
+  TENSOR(vp, 8, "fb_evict_kv", "v_pool", z[Z_FP8] ? T_U8 : T_BF16, z[Z_POOL], 1)
+  TENSOR(ws, 9, "fb_evict_kv", "ws", T_U8, z[Z_WS_EVICT], 1)
+  TENSOR(status, 10, "fb_evict_kv", "status", T_I32, 1, 1)
+  CALL(FN(F_EVICT, fb_evict_kv)(ctx, &kv, keep, recent, sinks, kp, vp, ws, status, stream))
+}
+
 #define M(name, f) {name, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {
     M("bind", bind), M("pack", m_pack), M("attn", m_attn), M("attn_fp8", m_attn8), M("t2t", m_t2t), M("gate", m_gate),
     M("scatter", m_scatter), M("scatter_fp8", m_scatter8), M("embed", m_embed), M("lm_head", m_head),
     M("attn_static", m_static), M("dtypes", dtypes), M("append", m_append), M("append_fp8", m_append8),
-    M("token_attn", m_token), M("token_attn_fp8", m_token8), {NULL, NULL, 0, NULL}};
+    M("token_attn", m_token), M("token_attn_fp8", m_token8), M("evict", m_evict), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the binding", -1, methods,
                                     NULL, NULL, NULL, NULL};
 

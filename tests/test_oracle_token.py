@@ -98,7 +98,8 @@ def test_eviction_keeps_the_heaviest_and_attention_sees_just_them():
     assert list(lens) == [6, 7, 0, 13]
     out, _ = O.token_attn(cfg, lens, table, q, kp, vp)
     for h in range(2):
-        order = sorted(range(20), key=lambda j: (not (p0[0, h, j] < 3 or p0[0, h, j] > 44), -w0[0, h, j], j))[:6]
+        safe = (p0[0, h] < 3) | (p0[0, h] > 44)
+        order = (list(np.flatnonzero(safe)) + [j for j in np.argsort(-w0[0, h], kind="stable") if not safe[j]])[:6]
         rows = lambda pool: O.stored_rows(cfg, lens0, table, pool, 0, h)[order]
         have = O.stored_rows(cfg, lens, table, kp, 0, h)
         np.testing.assert_array_equal(np.sort(have[:, 0]), np.sort(rows(k0)[:, 0]))

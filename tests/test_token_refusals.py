@@ -155,3 +155,50 @@ def test_token_attn_refuses_tensors_that_do_not_fit(monkeypatch):
             u["ws"] = torch.zeros(8, dtype=torch.uint8)
         with pytest.raises(ValueError, match="contiguous"):
             B.fb_token_attn(ctx, cache_tensors(), u["q"], u["pool"], u["pool"], u["out"], u["ws"], u["status"], u["acc"])
+
+
+def test_evict_refuses():
+    lib, ctx, ctx8 = B.lib(), B.Context(**GOOD), B.Context(**FP8)
+    call = lambda c, kv, *a: lib.fb_evict_kv(c.handle, kv and C.byref(kv), *a)
+    ok = [P, 16, 4, P, P, P, P, None]              # keep, recent, sinks, k_pool, v_pool, ws, status, stream
+    refused(ctx, call(ctx, None, *ok), B.FB_ERR_INVALID_ARG, b"cache is null")
+    for name in ("kv_len", "page_table"):
+        refused(ctx, call(ctx, with_null(name), *ok), B.FB_ERR_INVALID_ARG, b"cache.kv_len or cache.page_table")
+    for name in ("tok_pos", "kv_pos", "kv_weight"):
+        refused(ctx, call(ctx, with_null(name), *ok), B.FB_ERR_INVALID_ARG, b"cache.tok_pos, cache.kv_pos or cache.kv_weight")
+    for i in (0, 3, 4, 6):
+        a = list(ok)
+        a[i] = None
+        refused(ctx, call(ctx, full(), *a), B.FB_ERR_INVALID_ARG, b"null")
+    for i in (1, 2):
+        a = list(ok)
+        a[i] = -1
+        for c in (ctx, ctx8):
+            refused(c, call(c, full(), *a), B.FB_ERR_INVALID_ARG, b"recent and sinks")
+    a = list(ok)
+    a[5] = None
+    refused(ctx, call(ctx, full(), *a), B.FB_ERR_WORKSPACE, b"workspace is null")
+    for i in (3, 4, 5):
+        a = list(ok)
+        a[i] = P + 8
+        refused(ctx, call(ctx, full(), *a), B.FB_ERR_ALIGNMENT, b"aligned")
+    assert lib.fb_evict_kv(None, None, *ok) == B.FB_ERR_INVALID_ARG
+    assert lib.fb_evict_workspace_bytes(None) == 0 and lib.fb_evict_workspace_bytes(ctx.handle) > 0
+    wide = B.Context(**dict(GOOD, max_pages_per_req=1 << 25))
+    refused(wide, call(wide, full(), *ok), B.FB_ERR_UNSUPPORTED, b"2^31")
+
+
+def test_evict_refuses_tensors_that_do_not_fit(monkeypatch):
+    ctx, t = B.Context(**GOOD), tensors()
+    monkeypatch.setattr(B, "_device", lambda: -1)
+    monkeypatch.setattr(B, "_stream", lambda s: 0)
+    keep, ws = torch.zeros(4, dtype=torch.int32), torch.zeros(B.lib().fb_evict_workspace_bytes(ctx.handle), dtype=torch.uint8)
+    for bad in (dict(keep=keep[:3]), dict(keep=keep.long()), dict(keep=torch.zeros(8, dtype=torch.int32)[::2]), dict(ws=ws[:-1].clone()),
+                dict(ws=ws.view(torch.int32)), dict(pool=t["pool"].view(torch.int16)), dict(pool=torch.zeros(16, 2, 64, 128, dtype=torch.uint8)),
+                dict(status=t["status"].float())):
+        u = dict(dict(keep=keep, ws=ws, pool=t["pool"], status=t["status"]), **bad)
+        with pytest.raises(ValueError, match="contiguous"):
+            B.fb_evict_kv(ctx, cache_tensors(), u["keep"], 4, 2, u["pool"], u["pool"], u["ws"], u["status"])
+    for name in ("tok_pos", "kv_pos", "kv_weight"):
+        with pytest.raises(B.FlowBlockError, match="null"):
+            B.fb_evict_kv(ctx, cache_tensors(**{name: None}), keep, 4, 2, t["pool"], t["pool"], ws, t["status"])
