@@ -454,7 +454,8 @@ int fb_evict_kv(fb_ctx* ctx, const fb_cache* cache, const int32_t* keep, int32_t
   if (!keep || !k_pool || !v_pool || !status) return fail(ctx, FB_ERR_INVALID_ARG, "a tensor pointer is null");
   if (recent < 0 || sinks < 0) return fail(ctx, FB_ERR_INVALID_ARG, "recent and sinks must not be negative");
   if (!ws) return fail(ctx, FB_ERR_WORKSPACE, "workspace is null");
-  if (!aligned16(k_pool) || !aligned16(v_pool)) return fail(ctx, FB_ERR_ALIGNMENT, "tensor pointers must be 16-byte aligned");
+  if (!aligned16(k_pool) || !aligned16(v_pool) || !aligned16(cache->kv_pos) || !aligned16(cache->kv_weight))
+    return fail(ctx, FB_ERR_ALIGNMENT, "tensor pointers must be 16-byte aligned");
   if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(ctx, FB_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
   return fb::launch_evict(ctx, cache, keep, recent, sinks, k_pool, v_pool, ws, status, (cudaStream_t)stream);
 }

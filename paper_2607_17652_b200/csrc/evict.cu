@@ -5,11 +5,13 @@
 // with m = keep[r], the keys that stay at or above m take the places below m that become free, i-th to i-th.  Sources
 // and destinations do not overlap, so every row moves at once, and the caller's prefix of m keys is the whole cache.
 //
-// Kernel 1, a cluster of 1 to 8 CTAs per (request, KV head): the m-th largest rank by radix selection (11, 11 and 10
-// bits of a 32-bit key in shared-memory histograms; ranks are held in registers, 8,192 a CTA), then the lists of
-// freed places and of keys to move, both in index order by ballots and one scan.  Bound by its chain of
-// about ten block-wide steps; reads 8 bytes a stored key.
-// Kernel 2: the rows of K and V, the weights and the positions, eight moves a warp with their loads in flight.
+// Kernel 1, a cluster of 1 to 8 CTAs per (request, KV head): the rank of the last key that stays, by counting.  The range
+// of the ranks is cut into 512 bins, the bin that holds the boundary into 512 again, until all keys of a bin stay
+// (two or three times, 512 bins that follow the range spread the counts over many addresses); then the lists of freed
+// places and of keys to move, both in index order by ballots and one scan.  Bound by its chain of block-wide steps: loops
+// are kept short, since every CTA runs the code once, and what goes between the CTAs of a cluster is kept small (one request
+// of 28,123 keys: 11-bit digits, unrolled over keys in registers 23 us, this form FIGURE).  Reads 8 bytes a stored key.
+// Kernel 2: the rows of K and V, the weights and the positions, eight rows a warp under way.
 // HBM-bound where many move.
 #include <cooperative_groups.h>
 
@@ -19,11 +21,11 @@ namespace fb {
 
 namespace cg = cooperative_groups;
 
-constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
-constexpr int kSelPer = 16;                       // keys of a thread in registers
-constexpr int kSelCap = kSelThreads * kSelPer;    // ... of a CTA
-constexpr int kBins = 2048;
-constexpr int kMoveThreads = 256, kMoveBatch = 8;
+constexpr int kSelThreads = 256, kSelWarps = kSelThreads / 32;
+constexpr int kSelPer = 16;                       // keys of a thread
+constexpr int kSelCap = kSelThreads * kSelPer;    // ... of a CTA, in shared memory
+constexpr int kBinBits = 9, kBins = 1 << kBinBits, kMaxCluster = 8;
+constexpr int kMoveThreads = 256, kMoveWarps = kMoveThreads / 32, kMoveAhead = 8;
 
 struct EvictParams {
   int32_t *kv_len, *kv_pos;
@@ -36,21 +38,23 @@ struct EvictParams {
   int32_t n_kv_heads, max_pages_per_req, num_pages, recent, sinks;
 };
 
-// Rank of a key as an unsigned number: protected keys above all, a NaN below all, -0 as 0.
-__device__ __forceinline__ uint32_t rank_of(float w, int pos, int sinks, long long newest_out) {
-  if (pos < sinks || pos > newest_out) return 0xffffffffu;
-  if (w != w) return 0u;
+// Rank of a key as an unsigned number: protected keys above all, a NaN below all, -0 as 0.  `first`: the first of the last
+// `recent` positions.
+struct Guarded { int sinks, first; bool any; };
+__device__ __forceinline__ uint32_t rank_of(float w, int pos, const Guarded& g) {
   const uint32_t u = __float_as_uint(w + 0.f);
-  return u >> 31 ? ~u : u | 0x80000000u;
+  uint32_t k = u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
+  if (w != w) k = 0u;
+  return pos < g.sinks || (g.any && pos >= g.first) ? 0xffffffffu : k;
 }
 
-// Exclusive scan of kSelPer * kSelWarps packed pairs of 16-bit counts, in index order; returns the total.  All threads.
+// Exclusive scan of kSelPer * kSelWarps counts (or pairs of 16-bit counts) in index order; returns the total.  All threads.
 __device__ __forceinline__ uint32_t scan_counts(uint32_t* cnt, uint32_t* warp_sum) {
-  static_assert(kSelPer * kSelWarps == 256, "eight warps, a count a lane");
+  static_assert(kSelPer * kSelWarps == 128, "four warps, a count a lane");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   __syncthreads();
   uint32_t v = 0, incl = 0;
-  if (tid < 256) {
+  if (tid < 128) {
     v = incl = cnt[tid];
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -62,12 +66,12 @@ __device__ __forceinline__ uint32_t scan_counts(uint32_t* cnt, uint32_t* warp_su
   __syncthreads();
   uint32_t before = 0, total = 0;
 #pragma unroll
-  for (int w = 0; w < 8; ++w) {
+  for (int w = 0; w < 4; ++w) {
     const uint32_t x = warp_sum[w];
     before += w < warp ? x : 0;
     total += x;
   }
-  if (tid < 256) cnt[tid] = before + incl - v;
+  if (tid < 128) cnt[tid] = before + incl - v;
   __syncthreads();
   return total;
 }
@@ -76,197 +80,267 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const EvictPa
   cg::cluster_group cluster = cg::this_cluster();
   const int cl = (int)cluster.num_blocks(), me = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  __shared__ uint32_t hist[kBins];
+  __shared__ __align__(16) uint32_t key[kSelCap];  // weights, then ranks
+  __shared__ __align__(16) int32_t kpos[kSelCap];
+  __shared__ __align__(16) uint32_t hist[2][kBins];
   __shared__ uint32_t cnt[kSelPer * kSelWarps], warp_sum[kSelWarps];
-  __shared__ uint32_t found[2];                   // digit, keys still to be taken from it
-  __shared__ uint32_t mine[3];                    // equal keys; freed places; keys to move, of this CTA
+  __shared__ uint32_t found[3];                    // bin, keys still to be taken from it, keys in it
+  __shared__ uint32_t part[3][kSelWarps];
+  __shared__ uint32_t peer[3][4][kMaxCluster];     // what the CTAs of the cluster have told this one, by occasion
   pdl_wait_then_release();
   const int line = blockIdx.x / cl, r = line / p.n_kv_heads;
   const int n = p.kv_len[r], m = p.keep[r], newest = p.tok_pos[r];
-  const long long cap = (long long)p.max_pages_per_req * kPage, newest_out = (long long)newest - p.recent;
-  // (the same for all CTAs of the cluster up to here and to the barriers below)
+  const long long cap = (long long)p.max_pages_per_req * kPage;
+  const bool over = n > 0 && n <= cap && m >= 0 && n > m;
+  // this CTA's keys: [lo, hi), kSelCap at a time; a place of theirs in a chunk is k * kSelThreads + thread
+  const int span = over ? ((n + cl - 1) / cl + 3) & ~3 : 0, lo = min(n, me * span), hi = min(n, lo + span);
+  const size_t row = (size_t)line * cap;
+  const long long first = (long long)newest - p.recent + 1;
+  const Guarded guard{p.sinks, (int)max(first, -0x80000000ll), p.recent > 0};
+  // A chunk's weights and positions, four at a time and all under way at once (a row starts on 256 bytes and is whole pages
+  // long, so that the last four stay inside it); each thread turns what it has fetched into ranks.
+  uint32_t low = 0xffffffffu, high = 0, guards = 0; // of the unprotected ranks, and protected keys
+  auto load = [&](int base) {
+    const int quads = (min(hi - base, kSelCap) + 3) / 4;
+    for (int i = tid; i < quads; i += kSelThreads) {
+      const uint32_t a = (uint32_t)__cvta_generic_to_shared(key + 4 * i), b = (uint32_t)__cvta_generic_to_shared(kpos + 4 * i);
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(a), "l"(p.kv_weight + row + base + 4 * i) : "memory");
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(b), "l"(p.kv_pos + row + base + 4 * i) : "memory");
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    for (int i = tid; i < quads; i += kSelThreads) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t x = rank_of(__uint_as_float(key[4 * i + j]), kpos[4 * i + j], guard);
+        key[4 * i + j] = x;
+        if (base + 4 * i + j < hi) {
+          if (x == 0xffffffffu) ++guards;
+          else { low = min(low, x); high = max(high, x); }
+        }
+      }
+    }
+  };
   bool bad = false;
-  if (n > 0 && n <= cap && m >= 0 && n > m)
+  if (over) {
     for (int i = tid; i < (n + kPage - 1) / kPage; i += kSelThreads) {
       const int page = p.page_table[(size_t)r * p.max_pages_per_req + i];
       bad |= page < 0 || page >= p.num_pages;
     }
+    if (m > 0) load(lo);
+  }
   bad = __syncthreads_or(bad);
-  if (n <= 0 || n > cap || m < 0 || n <= m || bad || m == 0) {
+  // (the CTAs of a cluster leave together here or meet at all barriers below)
+  if (!over || bad || m == 0) {
     if (tid == 0 && me == 0) {
       if (n > cap) atomicOr(p.status, FB_ST_BAD_STATE);
       if (bad) atomicOr(p.status, FB_ST_BAD_PAGE);
-      p.info[line] = make_int2(0, n > 0 && n <= cap && m == 0 && !bad ? 0 : -1);
+      p.info[line] = make_int2(0, over && !bad ? 0 : -1);
     }
     return;
   }
-  // this CTA's keys: [lo, hi), those of a thread 512 apart; the first kSelCap stay in registers, the others are formed again
-  const int span = (n + cl - 1) / cl, lo = min(n, me * span), hi = min(n, lo + span);
-  const float* w = p.kv_weight + (size_t)line * cap;
-  const int32_t* pos = p.kv_pos + (size_t)line * cap;
-  auto rank_at = [&](int i) { return rank_of(w[i], pos[i], p.sinks, newest_out); };
-  uint32_t key[kSelPer];
+  if (cl > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");       // (this CTA is there: its shared memory may be written)
+  const bool chunked = hi - lo > kSelCap;          // (longer than the shared memory of the cluster: chunks are read again in every pass)
+  auto used = [&](int base) { return min(kSelPer, (hi - base + kSelThreads - 1) / kSelThreads); };
+  // every key of the CTA, with its index; a chunk other than the one in shared memory is loaded first
+  int held = lo;
+  auto fetch = [&](int base) {
+    if (held == base) return;
+    __syncthreads();
+    load(base);
+    held = base;
+    __syncthreads();
+  };
+  if (chunked)
+    for (int base = lo + kSelCap; base < hi; base += kSelCap) fetch(base);       // (for low, high and guards)
+
+  // a value of every CTA to every CTA: put down in the others' shared memory, read behind the barrier
+  auto tell = [&](int occasion, int which, uint32_t v) {
+    if (tid < cl) *cluster.map_shared_rank(&peer[occasion][which][me], tid) = v;
+  };
   {
-    float wv[kSelPer];
-    int pv[kSelPer];
-#pragma unroll
-    for (int k = 0; k < kSelPer; ++k) {
-      const int i = lo + k * kSelThreads + tid;
-      wv[k] = i < hi ? w[i] : 0.f;
-      pv[k] = i < hi ? pos[i] : 0;
+    low = __reduce_min_sync(0xffffffffu, low);
+    high = __reduce_max_sync(0xffffffffu, high);
+    guards = __reduce_add_sync(0xffffffffu, guards);
+    if (lane == 0) { part[0][warp] = low; part[1][warp] = high; part[2][warp] = guards; }
+    for (int i = tid; i < 2 * kBins; i += kSelThreads) hist[0][i] = 0;
+    __syncthreads();
+    low = __reduce_min_sync(0xffffffffu, part[0][lane % kSelWarps]);
+    high = __reduce_max_sync(0xffffffffu, part[1][lane % kSelWarps]);
+    guards = __reduce_add_sync(0xffffffffu, lane < kSelWarps ? part[2][lane] : 0u);
+    if (cl > 1) {
+      asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+      tell(0, 0, low); tell(0, 1, high); tell(0, 2, guards);
+      cluster.sync();
+      low = __reduce_min_sync(0xffffffffu, peer[0][0][lane % cl]);
+      high = __reduce_max_sync(0xffffffffu, peer[0][1][lane % cl]);
+      guards = __reduce_add_sync(0xffffffffu, lane < cl ? peer[0][2][lane] : 0u);
     }
-#pragma unroll
-    for (int k = 0; k < kSelPer; ++k) key[k] = rank_of(wv[k], pv[k], p.sinks, newest_out);
   }
-
-  // the m-th largest rank, digit by digit
-  uint32_t prefix = 0, need = (uint32_t)m;
+  // The boundary: a range of ranks from `least` on, of which all keys stay, or (then it is a single rank) the first `need` in
+  // index order; keys above it stay.
+  uint32_t least = 0xffffffffu, need = (uint32_t)m, same = guards;
+  if (need > guards) {                             // not among the protected keys alone
+    need -= guards;
+    least = low;
+    int bits = 32 - __clz((int)(high - low));      // ranks are low + [0, 2^bits)
 #pragma unroll 1
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 0 ? 32 : pass == 1 ? 21 : 10;
-    const uint32_t mask = pass == 2 ? 1023u : 2047u;
-    if (cl > 1) cluster.sync();                   // (the others have read the histogram of the pass before)
-    else __syncthreads();
-    for (int b = tid; b < kBins; b += kSelThreads) hist[b] = 0;
-    __syncthreads();
-    auto count = [&](uint32_t x) {
-      if (pass == 0 || (x >> above) == prefix) atomicAdd(&hist[(x >> shift) & mask], 1u);
-    };
-#pragma unroll
-    for (int k = 0; k < kSelPer; ++k)
-      if (lo + k * kSelThreads + tid < hi) count(key[k]);
-    for (int i = lo + kSelCap + tid; i < hi; i += kSelThreads) count(rank_at(i));
-    if (cl > 1) cluster.sync();
-    else __syncthreads();
-    // four bins a thread, the largest digits first
-    uint32_t c[4], sum = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) c[j] = 0;
-    for (int q = 0; q < cl; ++q) {
-      const uint32_t* h = cl > 1 ? cluster.map_shared_rank(hist, q) : hist;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) c[j] += h[kBins - 1 - (4 * tid + j)];
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sum += c[j];
-    uint32_t incl = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += x;
-    }
-    if (lane == 31) warp_sum[warp] = incl;
-    __syncthreads();
-    uint32_t before = 0;
-#pragma unroll
-    for (int v = 0; v < kSelWarps; ++v) before += v < warp ? warp_sum[v] : 0;
-    before += incl - sum;
-    if (before < need && need <= before + sum) {  // (one thread)
-      uint32_t left = need - before;
-      int j = 0;
-      while (left > c[j]) left -= c[j++];
-      found[0] = kBins - 1 - (4 * tid + j);
-      found[1] = left;
-    }
-    __syncthreads();
-    prefix = pass == 2 ? prefix << 10 | found[0] : prefix << 11 | found[0];
-    need = found[1];
-  }
-  // `prefix` is that rank; of the keys that have it the first `need` in index order stay
-  const uint32_t least = prefix;
-  if (tid == 0) mine[0] = hist[least & 1023u];
-  if (cl > 1) cluster.sync();
-  else __syncthreads();
-  uint32_t eq_base = 0;
-  for (int q = 0; q < me; ++q) eq_base += *cluster.map_shared_rank(&mine[0], q);
-
-  // which of a thread's keys stay, for kSelCap keys at a time in index order; then the places below m that become free and
-  // the keys at or above m that stay, numbered in index order
-  const uint32_t below = (1u << lane) - 1u;
-  auto stays = [&](const uint32_t (&x)[kSelPer], int base, uint32_t& eq_before) {
-    uint32_t bits = 0;
-#pragma unroll
-    for (int k = 0; k < kSelPer; ++k) {
-      const bool in = base + k * kSelThreads + tid < hi;
-      if (in && x[k] > least) bits |= 1u << k;
-      const uint32_t e = __ballot_sync(0xffffffffu, in && x[k] == least);
-      if (lane == 0) cnt[k * kSelWarps + warp] = __popc(e);
-    }
-    const uint32_t total = scan_counts(cnt, warp_sum);
-#pragma unroll
-    for (int k = 0; k < kSelPer; ++k) {
-      const bool e = base + k * kSelThreads + tid < hi && x[k] == least;
-      const uint32_t at = eq_before + cnt[k * kSelWarps + warp] + __popc(__ballot_sync(0xffffffffu, e) & below);
-      if (e && at < need) bits |= 1u << k;
-    }
-    __syncthreads();                              // (cnt is read no more)
-    eq_before += total;
-    return bits;
-  };
-  auto number = [&](uint32_t bits, int base, uint32_t& free_before, uint32_t& move_before, bool write) {
-#pragma unroll
-    for (int k = 0; k < kSelPer; ++k) {
-      const int i = base + k * kSelThreads + tid;
-      const uint32_t f = __ballot_sync(0xffffffffu, i < hi && i < m && !(bits >> k & 1));
-      const uint32_t v = __ballot_sync(0xffffffffu, i < hi && i >= m && (bits >> k & 1));
-      if (lane == 0) cnt[k * kSelWarps + warp] = __popc(f) | __popc(v) << 16;
-    }
-    const uint32_t total = scan_counts(cnt, warp_sum);
-    if (write) {
-      const size_t half = (size_t)(cap / 2);
-#pragma unroll
-      for (int k = 0; k < kSelPer; ++k) {
-        const int i = base + k * kSelThreads + tid;
-        const bool f = i < hi && i < m && !(bits >> k & 1), v = i < hi && i >= m && (bits >> k & 1);
-        const uint32_t bf = __ballot_sync(0xffffffffu, f), bv = __ballot_sync(0xffffffffu, v), c = cnt[k * kSelWarps + warp];
-        if (f) p.to[line * half + free_before + (c & 0xffffu) + __popc(bf & below)] = i;
-        if (v) p.from[line * half + move_before + (c >> 16) + __popc(bv & below)] = i;
+    for (int pass = 0;; ++pass) {
+      uint32_t* h = hist[pass & 1];
+      const int shift = max(0, bits - kBinBits);
+#pragma unroll 1
+      for (int base = lo; base < hi; base += kSelCap) {
+        fetch(base);
+        const int cnt_keys = min(hi - base, kSelCap);
+#pragma unroll 4
+        for (int i = tid; i < cnt_keys; i += kSelThreads) {
+          const uint32_t x = key[i] - least;
+          // (below the range: wraps around to a large number)
+          if (key[i] != 0xffffffffu && (bits == 32 || x >> bits == 0)) atomicAdd(&h[x >> shift], 1u);
+        }
       }
-    }
-    __syncthreads();
-    free_before += total & 0xffffu;
-    move_before += total >> 16;
-  };
-  auto ranks = [&](int base, uint32_t (&x)[kSelPer]) {
+      if (cl > 1) cluster.sync();
+      else __syncthreads();
+      // two bins a thread, the largest first
+      uint32_t c0 = 0, c1 = 0;
+      const int bin = kBins - 2 - 2 * tid;
+      if (cl == 1) {
+        const uint2 v = *reinterpret_cast<const uint2*>(h + bin);
+        c0 = v.y; c1 = v.x;
+      } else {
 #pragma unroll
-    for (int k = 0; k < kSelPer; ++k) {
-      const int i = base + k * kSelThreads + tid;
-      x[k] = base == lo ? key[k] : i < hi ? rank_at(i) : 0u;
+        for (int q = 0; q < kMaxCluster; ++q)
+          if (q < cl) {
+            const uint2 v = *reinterpret_cast<const uint2*>(cluster.map_shared_rank(h + bin, q));
+            c0 += v.y; c1 += v.x;
+          }
+      }
+      uint32_t incl = c0 + c1;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += x;
+      }
+      if (lane == 31) warp_sum[warp] = incl;
+      for (int i = tid; i < kBins; i += kSelThreads) hist[(pass & 1) ^ 1][i] = 0;       // (of the next pass; read by all in the one before)
+      __syncthreads();
+      uint32_t before = 0;
+#pragma unroll
+      for (int v = 0; v < kSelWarps; ++v) before += v < warp ? warp_sum[v] : 0;
+      before += incl - (c0 + c1);
+      if (before < need && need <= before + c0 + c1) {       // (one thread)
+        const bool second = need - before > c0;
+        found[0] = bin + (second ? 0 : 1);
+        found[1] = need - before - (second ? c0 : 0);
+        found[2] = second ? c1 : c0;
+      }
+      __syncthreads();
+      least += found[0] << shift;
+      need = found[1];
+      same = found[2];
+      bits = shift;
+      if (need == same || bits == 0) break;
     }
-  };
-  uint32_t first_free = 0, first_move = 0;        // (of the whole row, before this CTA's)
-  uint32_t eq0 = eq_base, bits0 = 0, x[kSelPer];
-  if (cl > 1) {
-    // the counts of every CTA first, the numbers of those before it, then the lists
-    uint32_t f = 0, v = 0, eq = eq_base;
+  }
+  const bool ties = need != same;                  // (then the range is one rank)
+  uint32_t eq_first = 0;
+  if (ties && cl > 1) {                            // equal keys of the CTAs before this one
+    uint32_t e = 0;
+#pragma unroll 1
     for (int base = lo; base < hi; base += kSelCap) {
-      ranks(base, x);
-      const uint32_t bits = stays(x, base, eq);
-      if (base == lo) { bits0 = bits; eq0 = eq; }
-      number(bits, base, f, v, false);
+      fetch(base);
+      for (int i = tid; i < min(hi - base, kSelCap); i += kSelThreads) e += key[i] == least;
     }
-    if (tid == 0) { mine[1] = f; mine[2] = v; }
+    e = __reduce_add_sync(0xffffffffu, e);
+    __syncthreads();
+    if (lane == 0) part[0][warp] = e;
+    __syncthreads();
+    tell(1, 0, __reduce_add_sync(0xffffffffu, lane < kSelWarps ? part[0][lane] : 0u));
     cluster.sync();
-    for (int q = 0; q < me; ++q) {
-      first_free += *cluster.map_shared_rank(&mine[1], q);
-      first_move += *cluster.map_shared_rank(&mine[2], q);
+    eq_first = __reduce_add_sync(0xffffffffu, lane < me ? peer[1][0][lane] : 0u);
+  }
+
+  // Twice over the CTA's keys: the counts, of which the CTAs behind it are told, then the lists.  (One chunk, whose numbers are
+  // still in cnt the second time, unless the row is chunked.)
+  const uint32_t below = (1u << lane) - 1u;
+  const size_t half = (size_t)(cap / 2);
+  uint32_t bits = 0, frees = 0, moves = 0, eq_before = eq_first;       // frees, moves: of the chunks gone through; in the second go with those of the CTAs before
+#pragma unroll 1
+  for (int go = 0; go < 2; ++go) {
+    if (go == 1) {
+      const uint32_t f = frees, v = moves;
+      frees = moves = 0;
+      if (cl > 1) {
+        tell(2, 0, f);
+        tell(2, 1, v);
+        cluster.sync();
+        frees = __reduce_add_sync(0xffffffffu, lane < me ? peer[2][0][lane] : 0u);
+        moves = __reduce_add_sync(0xffffffffu, lane < me ? peer[2][1][lane] : 0u);
+      }
+      if (me == cl - 1 && tid == 0) p.info[line] = make_int2((int)(frees + f), m);
+      eq_before = eq_first;
+    }
+#pragma unroll 1
+    for (int base = lo; base < hi; base += kSelCap) {
+      const int in = hi - base, ks = used(base);
+      uint32_t total = 0;
+      if (go == 0 || chunked) {
+        fetch(base);
+        bits = 0;                                  // bit k: the thread's k-th key stays
+        if (ties) {
+          for (int i = tid; i < kSelPer * kSelWarps; i += kSelThreads) cnt[i] = 0;
+          __syncthreads();
+#pragma unroll 1
+          for (int k = 0; k < ks; ++k) {
+            const int i = k * kSelThreads + tid;
+            const uint32_t e = __ballot_sync(0xffffffffu, i < in && key[i] == least);
+            if (lane == 0) cnt[k * kSelWarps + warp] = __popc(e);
+          }
+          const uint32_t equal = scan_counts(cnt, warp_sum);
+#pragma unroll 1
+          for (int k = 0; k < ks; ++k) {
+            const int i = k * kSelThreads + tid;
+            const bool e = i < in && key[i] == least;
+            const uint32_t at = eq_before + cnt[k * kSelWarps + warp] + __popc(__ballot_sync(0xffffffffu, e) & below);
+            if (i < in && (key[i] > least || (e && at < need))) bits |= 1u << k;
+          }
+          eq_before += equal;
+          __syncthreads();                         // (cnt is read no more)
+        } else {
+#pragma unroll 4
+          for (int k = 0; k < ks; ++k)
+            if (k * kSelThreads + tid < in && key[k * kSelThreads + tid] >= least) bits |= 1u << k;
+        }
+        for (int i = tid; i < kSelPer * kSelWarps; i += kSelThreads) cnt[i] = 0;
+        __syncthreads();
+#pragma unroll 2
+        for (int k = 0; k < ks; ++k) {             // places that become free (low half) and keys that move (high half)
+          const int i = k * kSelThreads + tid;
+          const bool s = bits >> k & 1;
+          const uint32_t f = __ballot_sync(0xffffffffu, i < in && base + i < m && !s), v = __ballot_sync(0xffffffffu, base + i >= m && s);
+          if (lane == 0) cnt[k * kSelWarps + warp] = __popc(f) | __popc(v) << 16;
+        }
+        total = scan_counts(cnt, warp_sum);
+      }
+      if (go == 1) {
+#pragma unroll 2
+        for (int k = 0; k < ks; ++k) {
+          const int i = k * kSelThreads + tid;
+          const bool s = bits >> k & 1, f = i < in && base + i < m && !s, v = base + i >= m && s;
+          const uint32_t bf = __ballot_sync(0xffffffffu, f), bv = __ballot_sync(0xffffffffu, v), c = cnt[k * kSelWarps + warp];
+          if (f) p.to[line * half + frees + (c & 0xffffu) + __popc(bf & below)] = base + i;
+          if (v) p.from[line * half + moves + (c >> 16) + __popc(bv & below)] = base + i;
+        }
+        __syncthreads();                           // (cnt is read no more)
+      }
+      frees += total & 0xffffu;
+      moves += total >> 16;
     }
   }
-  uint32_t f = first_free, v = first_move;
-  for (int base = lo; base < hi; base += kSelCap) {
-    uint32_t bits = bits0;
-    if (cl == 1 || base > lo) {
-      ranks(base, x);
-      bits = stays(x, base, eq0);
-    }
-    number(bits, base, f, v, true);
-  }
-  if (me == cl - 1 && tid == 0) p.info[line] = make_int2((int)f, m);
-  if (cl > 1) cluster.sync();                     // (what the others read stays until they have)
+  if (cl > 1) cluster.sync();                      // (no CTA leaves while another may read its histogram)
 }
 
-// kVec: 16-byte pieces of a stored row.  A warp takes eight moves: their places by its first eight lanes, then the rows, K and
-// V side by side, all loads before the first store.
+// kVec: 16-byte pieces of a stored row.  The warps of a line have equal contiguous shares of its moves, 32 places at a time by
+// their lanes and eight rows under way, K and V side by side.
 template <int kVec>
 __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictParams p) {
   pdl_wait();
@@ -281,30 +355,36 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictPar
   const int side = lane / (2 * kVec), in = lane % (2 * kVec);
   uint4* pool = in < kVec ? p.k_pool : p.v_pool;
   const int piece = in % kVec;
-  for (int i0 = (blockIdx.y * (kMoveThreads / 32) + warp) * kMoveBatch; i0 < info.x; i0 += gridDim.y * (kMoveThreads / 32) * kMoveBatch) {
-    const int n = min(kMoveBatch, info.x - i0);
+  const int warps = gridDim.y * kMoveWarps, share = max((info.x + warps - 1) / warps, kMoveAhead);
+  const long long begin = (long long)(blockIdx.y * kMoveWarps + warp) * share;
+  const int end = (int)min((long long)info.x, begin + share);
+  for (int i0 = (int)min(begin, (long long)info.x); i0 < end; i0 += 32) {
+    const int n = min(32, end - i0);
     long long dst = 0, src = 0;                   // rows
     if (lane < n) {
       const int to = p.to[list + i0 + lane], at = p.from[list + i0 + lane];
+      const int page_to = pages[to / kPage], page_at = pages[at / kPage];
       const float w = p.kv_weight[rec + at];
       const int ps = p.kv_pos[rec + at];
-      dst = ((long long)pages[to / kPage] * p.n_kv_heads + h) * kPage + to % kPage;
-      src = ((long long)pages[at / kPage] * p.n_kv_heads + h) * kPage + at % kPage;
+      dst = ((long long)page_to * p.n_kv_heads + h) * kPage + to % kPage;
+      src = ((long long)page_at * p.n_kv_heads + h) * kPage + at % kPage;
       p.kv_weight[rec + to] = w;
       p.kv_pos[rec + to] = ps;
     }
-    uint4 v[kMoveBatch / kSide];
+    for (int j0 = 0; j0 < n; j0 += kMoveAhead * kSide) {
+      uint4 v[kMoveAhead];
 #pragma unroll
-    for (int k = 0; k < kMoveBatch / kSide; ++k) {
-      const int j = k * kSide + side;
-      const long long s = __shfl_sync(0xffffffffu, src, j);
-      if (j < n) v[k] = pool[s * kVec + piece];
-    }
+      for (int k = 0; k < kMoveAhead; ++k) {
+        const int j = j0 + k * kSide + side;
+        const long long s = __shfl_sync(0xffffffffu, src, j);
+        if (j < n) v[k] = __ldcg(pool + s * kVec + piece);
+      }
 #pragma unroll
-    for (int k = 0; k < kMoveBatch / kSide; ++k) {
-      const int j = k * kSide + side;
-      const long long d = __shfl_sync(0xffffffffu, dst, j);
-      if (j < n) pool[d * kVec + piece] = v[k];
+      for (int k = 0; k < kMoveAhead; ++k) {
+        const int j = j0 + k * kSide + side;
+        const long long d = __shfl_sync(0xffffffffu, dst, j);
+        if (j < n) pool[d * kVec + piece] = v[k];
+      }
     }
   }
 }
@@ -336,14 +416,16 @@ int launch_evict(fb_ctx* ctx, const fb_cache* kv, const int32_t* keep, int recen
   p.n_kv_heads = c.n_kv_heads; p.max_pages_per_req = c.max_pages_per_req; p.num_pages = c.num_pages;
   p.recent = recent; p.sinks = sinks;
   const long long rows = (long long)c.max_requests * c.n_kv_heads, cap = (long long)c.max_pages_per_req * kPage;
+  // CTAs of a row: enough that its keys stay in registers, and more where rows are few (each has less to go through)
   int cl = 1;
-  while (cl < 8 && (long long)cl * kSelCap < cap) cl *= 2;
+  while (cl < 8 && cl * (long long)kSelCap < cap) cl *= 2;
+  while (cl < 8 && rows * cl * 2 <= kSms && cl * 512ll < cap) cl *= 2;
   if (rows * cl > 0x7fffffffll) return set_err(ctx, FB_ERR_UNSUPPORTED, "max_requests * n_kv_heads is too large");
   if (int e = cuda_err(ctx, launch_pdl_cluster(evict_select_kernel, dim3((unsigned)(rows * cl)), kSelThreads, 0, stream, cl, p),
                        "evict_select_kernel launch"))
     return e;
   // about eight CTAs an SM, no more than there can be batches
-  const long long batches = (cap / 2 + kMoveBatch * (kMoveThreads / 32) - 1) / (kMoveBatch * (kMoveThreads / 32)), want = 1 + 8 * kSms / rows;
+  const long long batch = kMoveAhead * kMoveWarps, batches = (cap / 2 + batch - 1) / batch, want = 1 + 8 * kSms / rows;
   const dim3 grid((unsigned)rows, (unsigned)(want < batches ? want : batches));
   const int row = c.head_dim * (c.kv_fp8 ? 1 : 2);
   return cuda_err(ctx, launch_pdl(row == 256 ? evict_move_kernel<16> : evict_move_kernel<8>, grid, kMoveThreads, 0, stream, p),

@@ -182,6 +182,10 @@ def test_evict_refuses():
         a = list(ok)
         a[i] = P + 8
         refused(ctx, call(ctx, full(), *a), B.FB_ERR_ALIGNMENT, b"aligned")
+    for name in ("kv_pos", "kv_weight"):
+        kv = full()
+        setattr(kv, name, P + 4)
+        refused(ctx, call(ctx, kv, *ok), B.FB_ERR_ALIGNMENT, b"16-byte")
     assert lib.fb_evict_kv(None, None, *ok) == B.FB_ERR_INVALID_ARG
     assert lib.fb_evict_workspace_bytes(None) == 0 and lib.fb_evict_workspace_bytes(ctx.handle) > 0
     wide = B.Context(**dict(GOOD, max_pages_per_req=1 << 25))
