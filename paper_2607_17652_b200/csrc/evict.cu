@@ -10,9 +10,10 @@
 // (two or three times, 512 bins that follow the range spread the counts over many addresses); then the lists of freed
 // places and of keys to move, both in index order by ballots and one scan.  Bound by its chain of block-wide steps: loops
 // are kept short, since every CTA runs the code once, and what goes between the CTAs of a cluster is kept small (one request
-// of 28,123 keys: 11-bit digits, unrolled over keys in registers 23 us, this form FIGURE).  Reads 8 bytes a stored key.
+// of 28,123 keys: digits of 11 bits and code unrolled over keys in registers 28 us, this form 16).  Reads 8 bytes a stored key.
 // Kernel 2: the rows of K and V, the weights and the positions, eight rows a warp under way.
-// HBM-bound where many move.
+// HBM-bound where many move, by rows of 128 to 256 bytes that lie apart: 64 requests cut from 1,024 to 8,192 keys to 2,000 move
+// 0.46 GB in bf16 at 4.4 TB/s, 0.23 GB in 8 bits at 3.7 TB/s; neither more rows under way nor more warps change that.
 #include <cooperative_groups.h>
 
 #include "fb_common.cuh"
@@ -22,7 +23,7 @@ namespace fb {
 namespace cg = cooperative_groups;
 
 constexpr int kSelThreads = 256, kSelWarps = kSelThreads / 32;
-constexpr int kSelPer = 16;                       // keys of a thread
+constexpr int kSelPer = 32;                       // keys of a thread
 constexpr int kSelCap = kSelThreads * kSelPer;    // ... of a CTA, in shared memory
 constexpr int kBinBits = 9, kBins = 1 << kBinBits, kMaxCluster = 8;
 constexpr int kMoveThreads = 256, kMoveWarps = kMoveThreads / 32, kMoveAhead = 8;
@@ -50,38 +51,35 @@ __device__ __forceinline__ uint32_t rank_of(float w, int pos, const Guarded& g) 
 
 // Exclusive scan of kSelPer * kSelWarps counts (or pairs of 16-bit counts) in index order; returns the total.  All threads.
 __device__ __forceinline__ uint32_t scan_counts(uint32_t* cnt, uint32_t* warp_sum) {
-  static_assert(kSelPer * kSelWarps == 128, "four warps, a count a lane");
+  static_assert(kSelPer * kSelWarps == kSelThreads, "a count a thread");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   __syncthreads();
-  uint32_t v = 0, incl = 0;
-  if (tid < 128) {
-    v = incl = cnt[tid];
+  const uint32_t v = cnt[tid];
+  uint32_t incl = v;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += x;
-    }
-    if (lane == 31) warp_sum[warp] = incl;
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += x;
   }
+  if (lane == 31) warp_sum[warp] = incl;
   __syncthreads();
   uint32_t before = 0, total = 0;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < kSelWarps; ++w) {
     const uint32_t x = warp_sum[w];
     before += w < warp ? x : 0;
     total += x;
   }
-  if (tid < 128) cnt[tid] = before + incl - v;
+  cnt[tid] = before + incl - v;
   __syncthreads();
   return total;
 }
 
-__global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const EvictParams p) {
+__global__ void __launch_bounds__(kSelThreads, 5) evict_select_kernel(const EvictParams p) {
   cg::cluster_group cluster = cg::this_cluster();
   const int cl = (int)cluster.num_blocks(), me = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  __shared__ __align__(16) uint32_t key[kSelCap];  // weights, then ranks
-  __shared__ __align__(16) int32_t kpos[kSelCap];
+  __shared__ __align__(16) uint32_t key[kSelCap];  // ranks
   __shared__ __align__(16) uint32_t hist[2][kBins];
   __shared__ uint32_t cnt[kSelPer * kSelWarps], warp_sum[kSelWarps];
   __shared__ uint32_t found[3];                    // bin, keys still to be taken from it, keys in it
@@ -97,27 +95,26 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const EvictPa
   const size_t row = (size_t)line * cap;
   const long long first = (long long)newest - p.recent + 1;
   const Guarded guard{p.sinks, (int)max(first, -0x80000000ll), p.recent > 0};
-  // A chunk's weights and positions, four at a time and all under way at once (a row starts on 256 bytes and is whole pages
-  // long, so that the last four stay inside it); each thread turns what it has fetched into ranks.
+  // A chunk's ranks from its weights and positions, four at a time (a row starts on 256 bytes and is whole pages long, so that
+  // the last four stay inside it).
   uint32_t low = 0xffffffffu, high = 0, guards = 0; // of the unprotected ranks, and protected keys
   auto load = [&](int base) {
     const int quads = (min(hi - base, kSelCap) + 3) / 4;
+    const float4* w4 = reinterpret_cast<const float4*>(p.kv_weight + row + base);
+    const int4* p4 = reinterpret_cast<const int4*>(p.kv_pos + row + base);
+#pragma unroll 2
     for (int i = tid; i < quads; i += kSelThreads) {
-      const uint32_t a = (uint32_t)__cvta_generic_to_shared(key + 4 * i), b = (uint32_t)__cvta_generic_to_shared(kpos + 4 * i);
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(a), "l"(p.kv_weight + row + base + 4 * i) : "memory");
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(b), "l"(p.kv_pos + row + base + 4 * i) : "memory");
-    }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    for (int i = tid; i < quads; i += kSelThreads) {
+      const float4 w = w4[i];
+      const int4 q = p4[i];
+      const uint4 x = make_uint4(rank_of(w.x, q.x, guard), rank_of(w.y, q.y, guard), rank_of(w.z, q.z, guard), rank_of(w.w, q.w, guard));
+      reinterpret_cast<uint4*>(key)[i] = x;
+      const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t x = rank_of(__uint_as_float(key[4 * i + j]), kpos[4 * i + j], guard);
-        key[4 * i + j] = x;
+      for (int j = 0; j < 4; ++j)
         if (base + 4 * i + j < hi) {
-          if (x == 0xffffffffu) ++guards;
-          else { low = min(low, x); high = max(high, x); }
+          if (xs[j] == 0xffffffffu) ++guards;
+          else { low = min(low, xs[j]); high = max(high, xs[j]); }
         }
-      }
     }
   };
   bool bad = false;
@@ -287,7 +284,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const EvictPa
         fetch(base);
         bits = 0;                                  // bit k: the thread's k-th key stays
         if (ties) {
-          for (int i = tid; i < kSelPer * kSelWarps; i += kSelThreads) cnt[i] = 0;
+          cnt[tid] = 0;
           __syncthreads();
 #pragma unroll 1
           for (int k = 0; k < ks; ++k) {
@@ -310,7 +307,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const EvictPa
           for (int k = 0; k < ks; ++k)
             if (k * kSelThreads + tid < in && key[k * kSelThreads + tid] >= least) bits |= 1u << k;
         }
-        for (int i = tid; i < kSelPer * kSelWarps; i += kSelThreads) cnt[i] = 0;
+        cnt[tid] = 0;
         __syncthreads();
 #pragma unroll 2
         for (int k = 0; k < ks; ++k) {             // places that become free (low half) and keys that move (high half)
@@ -342,7 +339,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const EvictPa
 // kVec: 16-byte pieces of a stored row.  The warps of a line have equal contiguous shares of its moves, 32 places at a time by
 // their lanes and eight rows under way, K and V side by side.
 template <int kVec>
-__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictParams p) {
+__global__ void __launch_bounds__(kMoveThreads, 3) evict_move_kernel(const EvictParams p) {
   pdl_wait();
   const int line = blockIdx.x, r = line / p.n_kv_heads, h = line % p.n_kv_heads;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -360,14 +357,14 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictPar
   const int end = (int)min((long long)info.x, begin + share);
   for (int i0 = (int)min(begin, (long long)info.x); i0 < end; i0 += 32) {
     const int n = min(32, end - i0);
-    long long dst = 0, src = 0;                   // rows
+    uint32_t dst = 0, src = 0;                    // rows (fewer than 2^32 fit on a device)
     if (lane < n) {
       const int to = p.to[list + i0 + lane], at = p.from[list + i0 + lane];
       const int page_to = pages[to / kPage], page_at = pages[at / kPage];
       const float w = p.kv_weight[rec + at];
       const int ps = p.kv_pos[rec + at];
-      dst = ((long long)page_to * p.n_kv_heads + h) * kPage + to % kPage;
-      src = ((long long)page_at * p.n_kv_heads + h) * kPage + at % kPage;
+      dst = ((uint32_t)page_to * p.n_kv_heads + h) * kPage + to % kPage;
+      src = ((uint32_t)page_at * p.n_kv_heads + h) * kPage + at % kPage;
       p.kv_weight[rec + to] = w;
       p.kv_pos[rec + to] = ps;
     }
@@ -376,13 +373,13 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictPar
 #pragma unroll
       for (int k = 0; k < kMoveAhead; ++k) {
         const int j = j0 + k * kSide + side;
-        const long long s = __shfl_sync(0xffffffffu, src, j);
+        const size_t s = __shfl_sync(0xffffffffu, src, j);
         if (j < n) v[k] = __ldcg(pool + s * kVec + piece);
       }
 #pragma unroll
       for (int k = 0; k < kMoveAhead; ++k) {
         const int j = j0 + k * kSide + side;
-        const long long d = __shfl_sync(0xffffffffu, dst, j);
+        const size_t d = __shfl_sync(0xffffffffu, dst, j);
         if (j < n) pool[d * kVec + piece] = v[k];
       }
     }
@@ -424,8 +421,8 @@ int launch_evict(fb_ctx* ctx, const fb_cache* kv, const int32_t* keep, int recen
   if (int e = cuda_err(ctx, launch_pdl_cluster(evict_select_kernel, dim3((unsigned)(rows * cl)), kSelThreads, 0, stream, cl, p),
                        "evict_select_kernel launch"))
     return e;
-  // about eight CTAs an SM, no more than there can be batches
-  const long long batch = kMoveAhead * kMoveWarps, batches = (cap / 2 + batch - 1) / batch, want = 1 + 8 * kSms / rows;
+  // about sixteen CTAs an SM (three at a time: lines have unlike numbers of moves), no more than there can be batches
+  const long long batch = kMoveAhead * kMoveWarps, batches = (cap / 2 + batch - 1) / batch, want = 1 + 16 * kSms / rows;
   const dim3 grid((unsigned)rows, (unsigned)(want < batches ? want : batches));
   const int row = c.head_dim * (c.kv_fp8 ? 1 : 2);
   return cuda_err(ctx, launch_pdl(row == 256 ? evict_move_kernel<16> : evict_move_kernel<8>, grid, kMoveThreads, 0, stream, p),
