@@ -88,16 +88,18 @@ class fb_device_bufs(C.Structure):
 # the calls that _marshal makes, in the order of its bind()
 _FAST = ("fb_pack_wavefronts", "fb_wavefront_attn", "fb_t2t_step", "fb_gate_commit", "fb_scatter_window_kv",
          "fb_scatter_window_kv_fp8", "fb_wavefront_attn_fp8", "fb_embed_gather", "fb_lm_head_t2t",
-         "fb_wavefront_attn_static", "fb_append_kv", "fb_append_kv_fp8", "fb_token_attn", "fb_token_attn_fp8",
-         "fb_evict_kv")
+         "fb_wavefront_attn_static")
+# ... and that _marshal_token makes
+_TOKEN = ("fb_append_kv", "fb_append_kv_fp8", "fb_token_attn", "fb_token_attn_fp8", "fb_evict_kv")
 
 _lib = None
 _m = None
+_mt = None
 
 
 def lib() -> C.CDLL:
     """The loaded CUDA library.  Raises if it is missing (no fallback)."""
-    global _lib, _m
+    global _lib, _m, _mt
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(
@@ -152,13 +154,16 @@ def lib() -> C.CDLL:
                          "fb_evict_workspace_bytes"):
                 getattr(l, n).restype = I
         try:
-            from . import _marshal
+            from . import _marshal, _marshal_token
         except ImportError as e:
-            raise RuntimeError("the marshalling module has not been built for this Python; run "
+            raise RuntimeError("the marshalling modules have not been built for this Python; run "
                                "`python -m paper_2607_17652_b200.build`") from e
-        _marshal.dtypes(torch.int32, torch.float32, torch.bfloat16, torch.uint8)
+        if _marshal_token.torch_version != torch.__version__.split("+")[0]:
+            raise RuntimeError("the marshalling module has been built for another torch; run "
+                               "`python -m paper_2607_17652_b200.build`")
+        _marshal_token.bind(*(C.cast(getattr(l, n), P).value for n in _TOKEN))
         _marshal.bind(*(C.cast(getattr(l, n), P).value for n in _FAST))
-        _lib, _m = l, _marshal
+        _lib, _m, _mt = l, _marshal, _marshal_token
     return _lib
 
 
@@ -204,7 +209,7 @@ class Context:
         if rc != FB_OK:
             raise FlowBlockError(rc, lib().fb_last_error(None).decode())
         self._hv = self._h.value
-        # what the calls that decode one token at a time hold their tensors against (csrc/marshal.c)
+        # what the calls that decode one token at a time hold their tensors against (csrc/marshal_token.cpp)
         c = self.cfg
         R, H, P = c.max_requests, c.n_kv_heads, c.max_pages_per_req
         self._sizes = (R, R * H * P * c.page_size, R * P, R * H * c.head_dim, R * c.n_q_heads * c.head_dim,
@@ -438,7 +443,7 @@ def fb_gate_commit(ctx: Context, pk: PackBuffers, slot_stats, st: DeviceState,
 def fb_append_kv(ctx: Context, cache: CacheState, k_new, v_new, k_pool, v_pool, status, rope_base: float = 0.0,
                  stream=None):
     """The newest token's K and V of every request to storage position kv_len - 1."""
-    rc = _m.append(ctx._hv, ctx._sizes, _device(), cache, k_new, v_new, k_pool, v_pool, rope_base, status, _stream(stream))
+    rc = _mt.append(ctx._hv, ctx._sizes, _device(), cache, k_new, v_new, k_pool, v_pool, rope_base, status, _stream(stream))
     if rc:
         ctx.check(rc)
 
@@ -446,7 +451,7 @@ def fb_append_kv(ctx: Context, cache: CacheState, k_new, v_new, k_pool, v_pool, 
 def fb_append_kv_fp8(ctx: Context, cache: CacheState, k_new, v_new, k_pool8, v_pool8, k_scale, v_scale, status,
                      rope_base: float = 0.0, stream=None):
     """The same into 8-bit (E4M3) pages."""
-    rc = _m.append_fp8(ctx._hv, ctx._sizes, _device(), cache, k_new, v_new, k_pool8, v_pool8, rope_base, status,
+    rc = _mt.append_fp8(ctx._hv, ctx._sizes, _device(), cache, k_new, v_new, k_pool8, v_pool8, rope_base, status,
                        _stream(stream), k_scale, v_scale)
     if rc:
         ctx.check(rc)
@@ -455,7 +460,7 @@ def fb_append_kv_fp8(ctx: Context, cache: CacheState, k_new, v_new, k_pool8, v_p
 def fb_token_attn(ctx: Context, cache: CacheState, q, k_pool, v_pool, out, ws, status, accumulate: bool = False,
                   stream=None):
     """One query token per request over all it has stored; ``accumulate``: its softmax weights are added to kv_weight."""
-    rc = _m.token_attn(ctx._hv, ctx._sizes, _device(), cache, q, k_pool, v_pool, out, accumulate, ws, status, _stream(stream))
+    rc = _mt.token_attn(ctx._hv, ctx._sizes, _device(), cache, q, k_pool, v_pool, out, accumulate, ws, status, _stream(stream))
     if rc:
         ctx.check(rc)
 
@@ -463,7 +468,7 @@ def fb_token_attn(ctx: Context, cache: CacheState, q, k_pool, v_pool, out, ws, s
 def fb_token_attn_fp8(ctx: Context, cache: CacheState, q, k_pool8, v_pool8, k_scale, v_scale, out, ws, status,
                       accumulate: bool = False, stream=None):
     """The same over 8-bit (E4M3) pages."""
-    rc = _m.token_attn_fp8(ctx._hv, ctx._sizes, _device(), cache, q, k_pool8, v_pool8, out, accumulate, ws, status,
+    rc = _mt.token_attn_fp8(ctx._hv, ctx._sizes, _device(), cache, q, k_pool8, v_pool8, out, accumulate, ws, status,
                            _stream(stream), k_scale, v_scale)
     if rc:
         ctx.check(rc)
@@ -472,7 +477,7 @@ def fb_token_attn_fp8(ctx: Context, cache: CacheState, q, k_pool8, v_pool8, k_sc
 def fb_evict_kv(ctx: Context, cache: CacheState, keep, recent: int, sinks: int, k_pool, v_pool, ws, status, stream=None):
     """Cuts every cache of more than keep[r] keys to that many: the last ``recent`` and the first ``sinks`` positions,
     then those of greatest accumulated weight.  bf16 or 8-bit pools, as the context says."""
-    rc = _m.evict(ctx._hv, ctx._sizes, _device(), cache, keep, recent, sinks, k_pool, v_pool, ws, status, _stream(stream))
+    rc = _mt.evict(ctx._hv, ctx._sizes, _device(), cache, keep, recent, sinks, k_pool, v_pool, ws, status, _stream(stream))
     if rc:
         ctx.check(rc)
 

@@ -1,11 +1,14 @@
 """Builds libflowblock.so (sm_100a) in-tree with nvcc, and the binding's
-marshalling module (csrc/marshal.c) with the C compiler.
+marshalling modules: csrc/marshal.c with the C compiler, csrc/marshal_token.cpp
+with the C++ compiler against the headers of the installed torch.
 
 ``python -m paper_2607_17652_b200.build`` or :func:`build`.  Cross-compiles
 without a GPU.  Objects are rebuilt only when a source or header is newer.
 """
 from __future__ import annotations
 
+import importlib.metadata
+import importlib.util
 import os
 import subprocess
 import sys
@@ -18,9 +21,9 @@ ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libflowblock.so")
 # named for the Python it is built against: another one does not load it
 MARSHAL = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
+MARSHAL_TOKEN = os.path.join(HERE, "_marshal_token" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.cu", "pack.cu", "t2t.cu", "gate_commit.cu", "attn_sm100.cu", "scatter.cu", "lm_head.cu",
-           "attn_static.cu", "attn_pair_sm100.cu", "token_attn.cu",
-           "evict.cu"]
+           "attn_static.cu", "attn_pair_sm100.cu", "token_attn.cu", "evict.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo",
               "-std=c++17", "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 
@@ -35,6 +38,23 @@ def _deps():
     hs = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))]
     hs.append(os.path.join(ROOT, "include", "flowblock.h"))
     return hs
+
+
+def _build_marshal_token(run, force: bool, hdr_time: float) -> None:
+    """Rebuilt for another torch too: it looks into torch's own structures."""
+    src, stamp = os.path.join(CSRC, "marshal_token.cpp"), os.path.join(HERE, "build", "marshal_token.torch")
+    version = importlib.metadata.version("torch")
+    same = os.path.exists(stamp) and open(stamp).read() == version
+    if not force and same and os.path.exists(MARSHAL_TOKEN) and \
+            os.path.getmtime(MARSHAL_TOKEN) >= max(os.path.getmtime(src), hdr_time):
+        return
+    torch_dir = importlib.util.find_spec("torch").submodule_search_locations[0]
+    inc, lib = os.path.join(torch_dir, "include"), os.path.join(torch_dir, "lib")
+    run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall",
+         "-I", sysconfig.get_paths()["include"], "-I", inc, "-I", os.path.join(inc, "torch", "csrc", "api", "include"),
+         "-L", lib, src, "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", MARSHAL_TOKEN])
+    with open(stamp, "w") as f:
+        f.write(version)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -71,6 +91,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
             os.path.getmtime(MARSHAL) < max(os.path.getmtime(src), hdr_time):
         run([os.environ.get("CC", "gcc"), "-O2", "-shared", "-fPIC", "-Wall",
              "-I", sysconfig.get_paths()["include"], src, "-o", MARSHAL])
+    _build_marshal_token(run, force, hdr_time)
     if logs:
         with open(os.path.join(HERE, "build", "ptxas.log"), "w") as f:
             f.write("\n".join(logs))
