@@ -102,6 +102,9 @@ __device__ __forceinline__ int tok_tiles(const TokenParams& p, int len, int tile
   return len > 0 && len <= (long long)p.max_pages_per_req * kPage ? (len + tile - 1) / tile : 0;
 }
 __device__ __forceinline__ int tok_len(const TokenParams& p, int r) { return r < p.requests ? __ldcg(p.kv_len + r) : 0; }
+__device__ __forceinline__ long long tok_div(long long a, long long b) {        // (both below 2^31 but in absurd contexts)
+  return (a | b) >> 31 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+}
 // Tiles of all rows (`total`) and of those of the requests before `upto`, and the share of a CTA: an equal one, but no
 // row in more than kMostPieces.  By a whole warp; `len`: the lane's length of the first 32 requests.
 constexpr int kMostPieces = 64;
@@ -126,7 +129,7 @@ __device__ __forceinline__ TokDeal tok_deal(const TokenParams& p, int tile, int 
   TokDeal d;
   d.total = all * rows;
   d.before = before * rows;
-  d.share = max((d.total + p.n_ctas - 1) / p.n_ctas, (long long)((longest + kMostPieces - 1) / kMostPieces));
+  d.share = max(tok_div(d.total + p.n_ctas - 1, p.n_ctas), (long long)((longest + kMostPieces - 1) / kMostPieces));
   return d;
 }
 // The pieces of a row: CTAs c0.. of the deal; a piece lies in slot 2 c + 1 where the row starts in that CTA, else in 2 c.
@@ -134,8 +137,8 @@ struct TokPieces {
   long long start, share;
   int c0, n;
   __device__ __forceinline__ TokPieces(long long start_, int nt, long long share_) : start(start_), share(share_) {
-    c0 = (int)(start / share);
-    n = (int)((start + nt - 1) / share) - c0 + 1;
+    c0 = (int)tok_div(start, share);
+    n = (int)tok_div(start + nt - 1, share) - c0 + 1;
   }
   __device__ __forceinline__ int slot(int i) const { return 2 * (c0 + i) + ((c0 + i) * share <= start ? 1 : 0); }
 };
@@ -155,14 +158,6 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
   const TokDeal deal = tok_deal(p, S::kTile, len, 0);
   long long at = (long long)blockIdx.x * deal.share;
   int left = (int)min(deal.share, deal.total - at > 0 ? deal.total - at : 0);
-  // rows without work: zeros where nothing is stored, a report where the length is no length
-  for (int r = blockIdx.x; r < p.requests; r += p.n_ctas) {
-    const int n = __ldcg(p.kv_len + r);
-    if (n > (long long)p.max_pages_per_req * kPage && tid == 0) atomicOr(p.status, FB_ST_BAD_STATE);
-    if (n != 0) continue;
-    uint4* o = reinterpret_cast<uint4*>(p.out) + (size_t)r * p.n_kv_heads * p.group * (D / 8);
-    for (int i = tid; i < p.n_kv_heads * p.group * (D / 8); i += kTokThreads) o[i] = make_uint4(0, 0, 0, 0);
-  }
   if (left <= 0) return;
   // the request that holds tile `at`, its length and tiles
   int r = 0, nt = 0;
@@ -187,7 +182,7 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
     at -= (long long)__shfl_sync(0xffffffffu, incl, 31) * rows;
   }
   if (nt == 0) return;                         // (not reached while nobody writes the lengths)
-  int row = (int)(at / nt), tile = (int)(at % nt);
+  int row = (int)tok_div(at, nt), tile = (int)(at - (long long)row * nt);
 
   while (true) {
     const int h = row / p.head_blocks, hb = row % p.head_blocks;
@@ -558,6 +553,15 @@ __global__ void __launch_bounds__(kTokThreads) token_join_kernel(const TokenPara
   // (the lengths are older than the stream kernel, which waited itself before it let this one start)
   const int first = tok_len(p, lane), len = tok_len(p, r), nt = tok_tiles(p, len, S::kTile);
   const bool idle = nt == 0 || (weights && hb != 0);
+  if (!weights && nt == 0 && blockIdx.y == 0) {  // zeros where nothing is stored, a report where the length is no length
+    if (len > 0 && row == 0 && tid == 0) atomicOr(p.status, FB_ST_BAD_STATE);
+    if (len == 0) {
+      pdl_wait_only();                           // (before that the stream's predecessors may still read or write the output)
+      const int heads = min(HB, p.group - hb * HB);
+      uint4* o = reinterpret_cast<uint4*>(p.out + (((size_t)r * p.n_kv_heads + h) * p.group + hb * HB) * D);
+      for (int i = tid; i < heads * (D / 8); i += kTokThreads) o[i] = make_uint4(0, 0, 0, 0);
+    }
+  }
   if (idle && !keeper) return;
   const TokDeal deal = tok_deal(p, S::kTile, first, r);
   const TokPieces k(deal.before + (long long)row * nt, nt, deal.share);
