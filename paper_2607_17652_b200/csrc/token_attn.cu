@@ -355,16 +355,18 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
         if constexpr (W) {
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
+            if (hb * HB + nb * 8 + 2 * t < p.group) {                // (this lane's heads of the block)
+              float* w = score + c * p.group + nb * 8 + 2 * t;
 #pragma unroll
-            for (int b = 0; b < S::kSub; ++b)
-#pragma unroll
-              for (int k = 0; k < 4; k += 2) {
-                const int j = b * 16 + (k >> 1) * 8 + c, g = nb * 8 + 2 * t;
-                if (j >= rem) continue;
-                float* w = score + j * p.group + g;
-                if (hb * HB + g + 1 < p.group) *reinterpret_cast<float2*>(w) = make_float2(s[nb][b][k], s[nb][b][k + 1]);
-                else if (hb * HB + g < p.group) *w = s[nb][b][k];
+              for (int b = 0; b < 2 * S::kSub; ++b) {
+                if (rem >= S::kKeys || b * 8 + c < rem) {
+                  const float x = s[nb][b >> 1][2 * (b & 1)], y = s[nb][b >> 1][2 * (b & 1) + 1];
+                  if (p.group > 1) *reinterpret_cast<float2*>(w) = make_float2(x, y);
+                  else *w = x;
+                }
+                w += 8 * p.group;
               }
+            }
         }
         if (__any_sync(0xffffffffu, move)) {     // rare after the first steps: the reference goes up to the largest score
 #pragma unroll
