@@ -269,6 +269,7 @@ struct fb_ctx {
   std::string err;
   float rope_base = 0.f;       // the base whose frequencies these are
   double inv_freq[64] = {};
+  int token_device = -1;       // device on which fb_token_attn has asked for clusters of sixteen
   // lazily initialised at the first attention launch
   bool dev_ready = false;
   int device = -1;        // the device the lazily initialised members belong to

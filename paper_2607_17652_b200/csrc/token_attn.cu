@@ -21,6 +21,7 @@
 // shared memory, no barrier, no address arithmetic but one base per step, and the next step's K and V are in flight
 // while this one's products run.  The tensor pipe (legacy mma.sync) is far from its rate: 4 d x 16 products a key
 // against 256 bytes from memory.
+#include <cooperative_groups.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
@@ -33,6 +34,8 @@ constexpr int kTokCtasPerSm = 3;         // (2 where a block has 16 heads: twice
 constexpr float kTokLog2e = 1.4426950408889634f;
 constexpr float kNoRef = -3.0e38f;       // below every score: the reference of a row that has seen no key
 constexpr float kRebase = 8.f;           // a score that far (in powers of two) above the reference moves it
+// fp16 weights start 2^7 above 1 (the reference lies that far below the score that set it), so that 2^-31 is still there
+template <bool F8> constexpr float kTokShift = F8 ? 7.f : 0.f;
 
 using bf16 = __nv_bfloat16;
 
@@ -51,6 +54,12 @@ struct TokenParams {
   int32_t requests, group, n_kv_heads, head_blocks, max_pages_per_req, num_pages, n_ctas, join_ctas;
   float sm_scale;
 };
+
+// Caches of at most kFewCapacity keys in at most kFewRows (request, KV head) rows take a cluster each, where no weights are
+// asked for.  us, dealt / a cluster each (32 query and 8 KV heads of 128, GPU time): one request of 200 keys 6.8 / 5.3, of 700 7.4 /
+// 5.9, of 3,001 9.0 / 8.1, of 8,192 14.5 / 14.2; 4 requests of 500 to 3,000 keys 12.2 / 11.3, of 1,000 to 8,192 18.9 / 20.9; 16
+// requests of 500 to 2,000 20.5 / 21.8; with weights one request of 3,001 9.1 / 10.5.  And one launch less for the host.
+constexpr int kFewCapacity = 4096, kFewRows = 32;
 
 // How keys are laid out over lanes and steps, by the bytes of a row.
 template <int D, bool F8>
@@ -144,15 +153,299 @@ struct TokPieces {
 };
 
 // ---------------------------------------------------------------- the stream
+// A warp's share of the keys of query heads [hb * 8 NB, ...) of (request r, KV head h): `steps` steps of S::kKeys keys from key
+// `first` on, kStep keys apart (0: step_), of the len that are stored.  Steps may lie behind them.  Leaves reference, sum (of this
+// lane's keys) and O^T in the lane's places.
+template <int D, bool F8, int NB, bool W, int kStep>
+__device__ __forceinline__ void tok_stream(const TokenParams& p, int r, int h, int hb, int len, int first, int steps, int step_,
+                                           float (&ref)[NB][2], float (&sum)[NB][2], float (&o)[NB][TokShape<D, F8>::kMb][4]) {
+  using S = TokShape<D, F8>;
+  constexpr int HB = 8 * NB;
+  constexpr float kShift = kTokShift<F8>;
+  const int lane = threadIdx.x & 31, c = lane >> 2, t = lane & 3, step = kStep ? kStep : step_;
+  // `rem` keys are stored from the step's first one on, `entry` is the page table's entry for it.  Its place inside a page is
+  // the same in every step (`step` is whole pages).
+  int rem = len - first;
+  const int in_page = first % kPage;
+  const int32_t* entry = p.page_table + (size_t)r * p.max_pages_per_req + first / kPage;
+  const size_t page_bytes = (size_t)p.n_kv_heads * kPage * S::kRow;
+  const size_t in_head = ((size_t)h * kPage + in_page) * S::kRow;
+  // the page of a step that is `ahead` steps on: only read where that step has keys
+  auto page_ahead = [&](int ahead) { return steps > ahead && rem > ahead * step ? __ldcg(entry + ahead * (step / kPage)) : 0; };
+  int page0 = page_ahead(0), page1 = page_ahead(1);
+  uint4 kr[8], vr[8];
+  // (n keys of the step are stored; what lies behind them is not read)
+  auto load_k = [&](size_t off, int n) {
+    const char* b = p.k_pool + off + c * S::kRow + t * 16;
+#pragma unroll
+    for (int s = 0; s < 2 * S::kSub; ++s)
+#pragma unroll
+      for (int u = 0; u < S::kU; ++u)
+        kr[s * S::kU + u] = n >= S::kKeys || s * 8 + c < n ? ld16(b + s * 8 * S::kRow + u * 64) : make_uint4(0, 0, 0, 0);
+  };
+  auto load_v = [&](size_t off, int n) {
+    const char* b = p.v_pool + off + 2 * t * S::kRow + c * 16;
+#pragma unroll
+    for (int s = 0; s < 4 * S::kSub; ++s)
+#pragma unroll
+      for (int u = 0; u < S::kV; ++u) {
+        const int key = (s >> 2) * 16 + (s & 1) + ((s >> 1) & 1) * 8;      // (+ 2t: this lane's)
+        vr[s * S::kV + u] = n >= S::kKeys || key + 2 * t < n ? ld16(b + key * S::kRow + u * 128) : make_uint4(0, 0, 0, 0);
+      }
+  };
+  auto inside = [&](int page) { return (unsigned)page < (unsigned)p.num_pages; };
+  // (the stream starts before the queries are looked at)
+  bool work = rem > 0 && inside(page0);
+  if (work) { load_k(page0 * page_bytes + in_head, rem); load_v(page0 * page_bytes + in_head, rem); }
+  // queries: head c of each block, in the order in which the lanes hold a key's row
+  uint32_t qf[NB][16 * S::kRow / 256 * (F8 ? 2 : 1)];
+  float fac[NB][2];
+  {
+    const float ks = F8 ? p.k_scale[h] : 1.f;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int g = hb * HB + nb * 8 + c;
+      const bf16* q = p.q + (((size_t)r * p.n_kv_heads + h) * p.group + g) * D;
+      constexpr int kQ = D / 32;             // 16-byte pieces of q a lane holds
+      uint4 v[kQ];
+#pragma unroll
+      for (int u = 0; u < kQ; ++u) {
+        // bf16 rows: piece u of lane t starts at 32 u + 8 t; 8-bit rows: 16 contiguous elements a load, two pieces
+        const int d0 = F8 ? (u >> 1) * 64 + t * 16 + (u & 1) * 8 : u * 32 + t * 8;
+        v[u] = g < p.group ? *reinterpret_cast<const uint4*>(q + d0) : make_uint4(0, 0, 0, 0);
+      }
+      float inv = 1.f;
+      if constexpr (F8) {
+        // fp16 after an exact scaling of the row by a power of two: its largest element comes to [2^15, 2^16)
+        float top = 0.f;
+#pragma unroll
+        for (int u = 0; u < kQ; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = word(v[u], i);
+            top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w << 16)), fabsf(__uint_as_float(w & 0xffff0000u))));
+          }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int e = top > 0.f ? min(126, 142 - (int)(__float_as_uint(top) >> 23)) : 0;
+        const float up = __uint_as_float((uint32_t)(127 + e) << 23);
+        inv = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+        for (int u = 0; u < kQ; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = word(v[u], i);
+            const __half2 x = __floats2half2_rn(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up);
+            qf[nb][u * 4 + i] = *reinterpret_cast<const uint32_t*>(&x);
+          }
+      } else {
+#pragma unroll
+        for (int u = 0; u < kQ; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) qf[nb][u * 4 + i] = word(v[u], i);
+      }
+      // scores in powers of two; a lane's columns of S^T are the heads 2t and 2t + 1
+      const float f = inv * ks * p.sm_scale * kTokLog2e;
+      fac[nb][0] = __shfl_sync(0xffffffffu, f, 8 * t);
+      fac[nb][1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) { ref[nb][j] = kNoRef; sum[nb][j] = 0.f; }
+#pragma unroll
+      for (int i = 0; i < S::kMb; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[nb][i][k] = 0.f;
+    }
+  }
+
+  [[maybe_unused]] float* score = nullptr;     // of this warp's first key of the step
+  if constexpr (W)
+    score = p.scores + (((size_t)r * p.n_kv_heads + h) * p.max_pages_per_req * kPage + first) * p.group + hb * HB;
+
+  for (; steps > 0; --steps) {
+    const bool work1 = steps > 1 && rem > step && inside(page1);
+    const size_t off1 = page1 * page_bytes + in_head;
+    const int page2 = page_ahead(2);
+    float s[NB][S::kSub][4];
+    if (work) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int b = 0; b < S::kSub; ++b)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) s[nb][b][k] = 0.f;
+#pragma unroll
+      for (int b = 0; b < S::kSub; ++b)
+#pragma unroll
+        for (int u = 0; u < S::kU; ++u) {
+          const uint4 lo = kr[(2 * b) * S::kU + u], hi = kr[(2 * b + 1) * S::kU + u];
+          if constexpr (F8) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t a[4];
+              e4m3x4_to_f16(word(lo, i), a[0], a[2]);
+              e4m3x4_to_f16(word(hi, i), a[1], a[3]);
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) mma16816<F8>(s[nb][b], a, qf[nb][(u * 4 + i) * 2], qf[nb][(u * 4 + i) * 2 + 1]);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t a[4] = {word(lo, 2 * i), word(hi, 2 * i), word(lo, 2 * i + 1), word(hi, 2 * i + 1)};
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) mma16816<F8>(s[nb][b], a, qf[nb][u * 4 + 2 * i], qf[nb][u * 4 + 2 * i + 1]);
+            }
+          }
+        }
+    }
+    if (work1) load_k(off1, rem - step);
+    if (rem > 0 && !work) {                    // a page outside the pool: its keys are left out
+      if (lane == 0) atomicOr(p.status, FB_ST_BAD_PAGE);
+      if constexpr (W)                         // (the scores of every stored position are read again)
+        for (int i = lane; i < min(rem, S::kKeys) * HB; i += 32)
+          if (hb * HB + i % HB < p.group) score[(size_t)(i / HB) * p.group + i % HB] = -INFINITY;
+    }
+    if (work) {
+      bool move = false;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          // rows c and c + 8 of each block of keys, head 2t + j
+          float top = kNoRef;
+#pragma unroll
+          for (int b = 0; b < S::kSub; ++b) {
+            s[nb][b][j] *= fac[nb][j];
+            s[nb][b][j + 2] *= fac[nb][j];
+            if (rem < S::kKeys) {
+              if (b * 16 + c >= rem) s[nb][b][j] = -INFINITY;
+              if (b * 16 + 8 + c >= rem) s[nb][b][j + 2] = -INFINITY;
+            }
+            top = fmaxf(top, fmaxf(s[nb][b][j], s[nb][b][j + 2]));
+          }
+          move |= top > ref[nb][j] + (kRebase + kShift);
+        }
+      if constexpr (W) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+          if (hb * HB + nb * 8 + 2 * t < p.group) {                // (this lane's heads of the block)
+            float* w = score + c * p.group + nb * 8 + 2 * t;
+#pragma unroll
+            for (int b = 0; b < 2 * S::kSub; ++b) {
+              if (rem >= S::kKeys || b * 8 + c < rem) {
+                const float x = s[nb][b >> 1][2 * (b & 1)], y = s[nb][b >> 1][2 * (b & 1) + 1];
+                if (p.group > 1) *reinterpret_cast<float2*>(w) = make_float2(x, y);
+                else *w = x;
+              }
+              w += 8 * p.group;
+            }
+          }
+      }
+      if (__any_sync(0xffffffffu, move)) {     // rare after the first steps: the reference goes up to the largest score
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            float m = ref[nb][j] + kShift;
+#pragma unroll
+            for (int b = 0; b < S::kSub; ++b) m = fmaxf(m, fmaxf(s[nb][b][j], s[nb][b][j + 2]));
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+            m -= kShift;
+            const float f = ex2(ref[nb][j] - m);
+            ref[nb][j] = m;
+            sum[nb][j] *= f;
+#pragma unroll
+            for (int i = 0; i < S::kMb; ++i) { o[nb][i][j] *= f; o[nb][i][j + 2] *= f; }
+          }
+      }
+      uint32_t pt[NB][S::kSub][2];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int b = 0; b < S::kSub; ++b)
+#pragma unroll
+          for (int k = 0; k < 4; k += 2) {
+            const float p0 = ex2(s[nb][b][k] - ref[nb][0]), p1 = ex2(s[nb][b][k + 1] - ref[nb][1]);
+            sum[nb][0] += p0;                  // (the sums are of the weights before they are rounded)
+            sum[nb][1] += p1;
+            uint32_t two;
+            if constexpr (F8) { const __half2 x = __floats2half2_rn(p0, p1); two = *reinterpret_cast<const uint32_t*>(&x); }
+            else { const __nv_bfloat162 x = __floats2bfloat162_rn(p0, p1); two = *reinterpret_cast<const uint32_t*>(&x); }
+            pt[nb][b][k >> 1] = transpose8x8(two);
+          }
+#pragma unroll
+      for (int b = 0; b < S::kSub; ++b)
+#pragma unroll
+        for (int i = 0; i < S::kMb; ++i) {
+          // rows of O^T: d = 8c + i and 64 + 8c + i (256-byte rows), 8c + 2i and the next (128-byte bf16), 16c + 2i and the next (8-bit)
+          uint32_t a[4];
+          if constexpr (F8) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const uint32_t w0 = word(vr[b * 4 + 2 * k], i >> 1), w1 = word(vr[b * 4 + 2 * k + 1], i >> 1);
+              e4m3x4_to_f16(__byte_perm(w0, w1, i & 1 ? 0x7362 : 0x5140), a[2 * k], a[2 * k + 1]);
+            }
+          } else if constexpr (D == 128) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int u = 0; u < 2; ++u)
+                a[2 * k + u] = __byte_perm(word(vr[(b * 4 + 2 * k) * 2 + u], i >> 1), word(vr[(b * 4 + 2 * k + 1) * 2 + u], i >> 1),
+                                           i & 1 ? 0x7632 : 0x5410);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const uint32_t w0 = word(vr[b * 4 + 2 * k], i), w1 = word(vr[b * 4 + 2 * k + 1], i);
+              a[2 * k] = __byte_perm(w0, w1, 0x5410);
+              a[2 * k + 1] = __byte_perm(w0, w1, 0x7632);
+            }
+          }
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) mma16816<F8>(o[nb][i], a, pt[nb][b][0], pt[nb][b][1]);
+        }
+    }
+    if (work1) load_v(off1, rem - step);
+    work = work1;
+    page1 = page2;
+    rem -= step;
+    entry += step / kPage;
+    if constexpr (W) score += step * p.group;
+  }
+}
+
+// A warp's results to shared memory: reference and sum of every head, O as [head][D + 1].
+template <int D, bool F8, int NB>
+__device__ __forceinline__ void tok_put(const float (&ref)[NB][2], const float (&sum)[NB][2], const float (&o)[NB][TokShape<D, F8>::kMb][4],
+                                        float2* ml, float* to) {
+  using S = TokShape<D, F8>;
+  const int lane = threadIdx.x & 31, c = lane >> 2, t = lane & 3;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float l = sum[nb][j];
+#pragma unroll
+      for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+      const int g = nb * 8 + 2 * t + j;
+      if (c == 0) ml[g] = make_float2(ref[nb][j], l);
+#pragma unroll
+      for (int i = 0; i < S::kMb; ++i) {
+        const int lo = F8 ? 16 * c + 2 * i : D == 128 ? 8 * c + i : 8 * c + 2 * i;
+        const int hi = !F8 && D == 128 ? 64 + lo : lo + 1;
+        to[g * (D + 1) + lo] = o[nb][i][j];
+        to[g * (D + 1) + hi] = o[nb][i][j + 2];
+      }
+    }
+}
+
 template <int D, bool F8, int NB, bool W>
 __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kernel(const TokenParams p) {
   using S = TokShape<D, F8>;
   constexpr int HB = 8 * NB, kStride = D + 1;
-  constexpr float kShift = F8 ? 7.f : 0.f;     // fp16 weights start 2^7 above 1 (the reference lies that far below), so that 2^-31 is still there
   __shared__ float sh_o[kTokWarps][HB * kStride];
   __shared__ float2 sh_ml[kTokWarps][HB];
   pdl_wait_then_release();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c = lane >> 2, t = lane & 3;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rows = p.n_kv_heads * p.head_blocks;
   int len = tok_len(p, lane);
   const TokDeal deal = tok_deal(p, S::kTile, len, 0);
@@ -187,277 +480,11 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
   while (true) {
     const int h = row / p.head_blocks, hb = row % p.head_blocks;
     const int seg = min(left, nt - tile), tile_end = tile + seg;
-    // Steps of this warp: `rem` keys are stored from its first one on, `entry` is the page table's entry for it; a step
-    // is S::kTile keys on.  Its place inside a page is the same in every step (a tile is whole pages).
-    constexpr int kPagesPerTile = S::kTile / kPage;
-    const int in_page = warp * S::kKeys % kPage;
-    int rem = len - (tile * S::kTile + warp * S::kKeys);
-    const int32_t* entry = p.page_table + (size_t)r * p.max_pages_per_req + tile * kPagesPerTile + warp * S::kKeys / kPage;
-    const int last_rem = len - ((tile_end - 1) * S::kTile + warp * S::kKeys);       // (of the segment's last step)
-    const size_t page_bytes = (size_t)p.n_kv_heads * kPage * S::kRow;
-    const size_t in_head = ((size_t)h * kPage + in_page) * S::kRow;
-    // the page of a step that is `ahead` steps on: only read where that step has keys
-    auto page_ahead = [&](int ahead) { return rem - ahead * S::kTile >= last_rem && rem - ahead * S::kTile > 0 ? __ldcg(entry + ahead * kPagesPerTile) : 0; };
-    int page0 = page_ahead(0), page1 = page_ahead(1);
-    uint4 kr[8], vr[8];
-    // (n keys of the step are stored; what lies behind them is not read)
-    auto load_k = [&](size_t off, int n) {
-      const char* b = p.k_pool + off + c * S::kRow + t * 16;
-#pragma unroll
-      for (int s = 0; s < 2 * S::kSub; ++s)
-#pragma unroll
-        for (int u = 0; u < S::kU; ++u)
-          kr[s * S::kU + u] = n >= S::kKeys || s * 8 + c < n ? ld16(b + s * 8 * S::kRow + u * 64) : make_uint4(0, 0, 0, 0);
-    };
-    auto load_v = [&](size_t off, int n) {
-      const char* b = p.v_pool + off + 2 * t * S::kRow + c * 16;
-#pragma unroll
-      for (int s = 0; s < 4 * S::kSub; ++s)
-#pragma unroll
-        for (int u = 0; u < S::kV; ++u) {
-          const int key = (s >> 2) * 16 + (s & 1) + ((s >> 1) & 1) * 8;      // (+ 2t: this lane's)
-          vr[s * S::kV + u] = n >= S::kKeys || key + 2 * t < n ? ld16(b + key * S::kRow + u * 128) : make_uint4(0, 0, 0, 0);
-        }
-    };
-    auto inside = [&](int page) { return (unsigned)page < (unsigned)p.num_pages; };
-    // (the stream starts before the queries are looked at)
-    bool work = rem > 0 && inside(page0);
-    if (work) { load_k(page0 * page_bytes + in_head, rem); load_v(page0 * page_bytes + in_head, rem); }
-    // queries: head c of each block, in the order in which the lanes hold a key's row
-    uint32_t qf[NB][16 * S::kRow / 256 * (F8 ? 2 : 1)];
-    float fac[NB][2];
-    float ref[NB][2], sum[NB][2];
-    float o[NB][S::kMb][4];
-    {
-      const float ks = F8 ? p.k_scale[h] : 1.f;
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const int g = hb * HB + nb * 8 + c;
-        const bf16* q = p.q + (((size_t)r * p.n_kv_heads + h) * p.group + g) * D;
-        constexpr int kQ = D / 32;             // 16-byte pieces of q a lane holds
-        uint4 v[kQ];
-#pragma unroll
-        for (int u = 0; u < kQ; ++u) {
-          // bf16 rows: piece u of lane t starts at 32 u + 8 t; 8-bit rows: 16 contiguous elements a load, two pieces
-          const int d0 = F8 ? (u >> 1) * 64 + t * 16 + (u & 1) * 8 : u * 32 + t * 8;
-          v[u] = g < p.group ? *reinterpret_cast<const uint4*>(q + d0) : make_uint4(0, 0, 0, 0);
-        }
-        float inv = 1.f;
-        if constexpr (F8) {
-          // fp16 after an exact scaling of the row by a power of two: its largest element comes to [2^15, 2^16)
-          float top = 0.f;
-#pragma unroll
-          for (int u = 0; u < kQ; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t w = word(v[u], i);
-              top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w << 16)), fabsf(__uint_as_float(w & 0xffff0000u))));
-            }
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          const int e = top > 0.f ? min(126, 142 - (int)(__float_as_uint(top) >> 23)) : 0;
-          const float up = __uint_as_float((uint32_t)(127 + e) << 23);
-          inv = __uint_as_float((uint32_t)(127 - e) << 23);
-#pragma unroll
-          for (int u = 0; u < kQ; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t w = word(v[u], i);
-              const __half2 x = __floats2half2_rn(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up);
-              qf[nb][u * 4 + i] = *reinterpret_cast<const uint32_t*>(&x);
-            }
-        } else {
-#pragma unroll
-          for (int u = 0; u < kQ; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) qf[nb][u * 4 + i] = word(v[u], i);
-        }
-        // scores in powers of two; a lane's columns of S^T are the heads 2t and 2t + 1
-        const float f = inv * ks * p.sm_scale * kTokLog2e;
-        fac[nb][0] = __shfl_sync(0xffffffffu, f, 8 * t);
-        fac[nb][1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) { ref[nb][j] = kNoRef; sum[nb][j] = 0.f; }
-#pragma unroll
-        for (int i = 0; i < S::kMb; ++i)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) o[nb][i][k] = 0.f;
-      }
-    }
+    float ref[NB][2], sum[NB][2], o[NB][S::kMb][4];
+    tok_stream<D, F8, NB, W, S::kTile>(p, r, h, hb, len, tile * S::kTile + warp * S::kKeys, seg, 0, ref, sum, o);
+    tile = tile_end;
 
-    [[maybe_unused]] float* score = nullptr;     // of this warp's first key of the step
-    if constexpr (W)
-      score = p.scores + (((size_t)r * p.n_kv_heads + h) * p.max_pages_per_req * kPage + tile * S::kTile + warp * S::kKeys) * p.group + hb * HB;
-
-    for (; tile < tile_end; ++tile) {
-      const bool more = tile + 1 < tile_end, work1 = more && rem > S::kTile && inside(page1);
-      const size_t off1 = page1 * page_bytes + in_head;
-      const int page2 = page_ahead(2);
-      float s[NB][S::kSub][4];
-      if (work) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int b = 0; b < S::kSub; ++b)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) s[nb][b][k] = 0.f;
-#pragma unroll
-        for (int b = 0; b < S::kSub; ++b)
-#pragma unroll
-          for (int u = 0; u < S::kU; ++u) {
-            const uint4 lo = kr[(2 * b) * S::kU + u], hi = kr[(2 * b + 1) * S::kU + u];
-            if constexpr (F8) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                uint32_t a[4];
-                e4m3x4_to_f16(word(lo, i), a[0], a[2]);
-                e4m3x4_to_f16(word(hi, i), a[1], a[3]);
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) mma16816<F8>(s[nb][b], a, qf[nb][(u * 4 + i) * 2], qf[nb][(u * 4 + i) * 2 + 1]);
-              }
-            } else {
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const uint32_t a[4] = {word(lo, 2 * i), word(hi, 2 * i), word(lo, 2 * i + 1), word(hi, 2 * i + 1)};
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) mma16816<F8>(s[nb][b], a, qf[nb][u * 4 + 2 * i], qf[nb][u * 4 + 2 * i + 1]);
-              }
-            }
-          }
-      }
-      if (work1) load_k(off1, rem - S::kTile);
-      if (rem > 0 && !work) {                    // a page outside the pool: its keys are left out
-        if (lane == 0) atomicOr(p.status, FB_ST_BAD_PAGE);
-        if constexpr (W)                         // (the scores of every stored position are read again)
-          for (int i = lane; i < min(rem, S::kKeys) * HB; i += 32)
-            if (hb * HB + i % HB < p.group) score[(size_t)(i / HB) * p.group + i % HB] = -INFINITY;
-      }
-      if (work) {
-        bool move = false;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            // rows c and c + 8 of each block of keys, head 2t + j
-            float top = kNoRef;
-#pragma unroll
-            for (int b = 0; b < S::kSub; ++b) {
-              s[nb][b][j] *= fac[nb][j];
-              s[nb][b][j + 2] *= fac[nb][j];
-              if (rem < S::kKeys) {
-                if (b * 16 + c >= rem) s[nb][b][j] = -INFINITY;
-                if (b * 16 + 8 + c >= rem) s[nb][b][j + 2] = -INFINITY;
-              }
-              top = fmaxf(top, fmaxf(s[nb][b][j], s[nb][b][j + 2]));
-            }
-            move |= top > ref[nb][j] + (kRebase + kShift);
-          }
-        if constexpr (W) {
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-            if (hb * HB + nb * 8 + 2 * t < p.group) {                // (this lane's heads of the block)
-              float* w = score + c * p.group + nb * 8 + 2 * t;
-#pragma unroll
-              for (int b = 0; b < 2 * S::kSub; ++b) {
-                if (rem >= S::kKeys || b * 8 + c < rem) {
-                  const float x = s[nb][b >> 1][2 * (b & 1)], y = s[nb][b >> 1][2 * (b & 1) + 1];
-                  if (p.group > 1) *reinterpret_cast<float2*>(w) = make_float2(x, y);
-                  else *w = x;
-                }
-                w += 8 * p.group;
-              }
-            }
-        }
-        if (__any_sync(0xffffffffu, move)) {     // rare after the first steps: the reference goes up to the largest score
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              float m = ref[nb][j] + kShift;
-#pragma unroll
-              for (int b = 0; b < S::kSub; ++b) m = fmaxf(m, fmaxf(s[nb][b][j], s[nb][b][j + 2]));
-#pragma unroll
-              for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-              m -= kShift;
-              const float f = ex2(ref[nb][j] - m);
-              ref[nb][j] = m;
-              sum[nb][j] *= f;
-#pragma unroll
-              for (int i = 0; i < S::kMb; ++i) { o[nb][i][j] *= f; o[nb][i][j + 2] *= f; }
-            }
-        }
-        uint32_t pt[NB][S::kSub][2];
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int b = 0; b < S::kSub; ++b)
-#pragma unroll
-            for (int k = 0; k < 4; k += 2) {
-              const float p0 = ex2(s[nb][b][k] - ref[nb][0]), p1 = ex2(s[nb][b][k + 1] - ref[nb][1]);
-              sum[nb][0] += p0;                  // (the sums are of the weights before they are rounded)
-              sum[nb][1] += p1;
-              uint32_t two;
-              if constexpr (F8) { const __half2 x = __floats2half2_rn(p0, p1); two = *reinterpret_cast<const uint32_t*>(&x); }
-              else { const __nv_bfloat162 x = __floats2bfloat162_rn(p0, p1); two = *reinterpret_cast<const uint32_t*>(&x); }
-              pt[nb][b][k >> 1] = transpose8x8(two);
-            }
-#pragma unroll
-        for (int b = 0; b < S::kSub; ++b)
-#pragma unroll
-          for (int i = 0; i < S::kMb; ++i) {
-            // rows of O^T: d = 8c + i and 64 + 8c + i (256-byte rows), 8c + 2i and the next (128-byte bf16), 16c + 2i and the next (8-bit)
-            uint32_t a[4];
-            if constexpr (F8) {
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const uint32_t w0 = word(vr[b * 4 + 2 * k], i >> 1), w1 = word(vr[b * 4 + 2 * k + 1], i >> 1);
-                e4m3x4_to_f16(__byte_perm(w0, w1, i & 1 ? 0x7362 : 0x5140), a[2 * k], a[2 * k + 1]);
-              }
-            } else if constexpr (D == 128) {
-#pragma unroll
-              for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-                  a[2 * k + u] = __byte_perm(word(vr[(b * 4 + 2 * k) * 2 + u], i >> 1), word(vr[(b * 4 + 2 * k + 1) * 2 + u], i >> 1),
-                                             i & 1 ? 0x7632 : 0x5410);
-            } else {
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const uint32_t w0 = word(vr[b * 4 + 2 * k], i), w1 = word(vr[b * 4 + 2 * k + 1], i);
-                a[2 * k] = __byte_perm(w0, w1, 0x5410);
-                a[2 * k + 1] = __byte_perm(w0, w1, 0x7632);
-              }
-            }
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) mma16816<F8>(o[nb][i], a, pt[nb][b][0], pt[nb][b][1]);
-          }
-      }
-      if (work1) load_v(off1, rem - S::kTile);
-      work = work1;
-      page1 = page2;
-      rem -= S::kTile;
-      entry += kPagesPerTile;
-      if constexpr (W) score += S::kTile * p.group;
-    }
-
-    // the four warps' shares of the segment, added in order
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float l = sum[nb][j];
-#pragma unroll
-        for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-        const int g = nb * 8 + 2 * t + j;
-        if (c == 0) sh_ml[warp][g] = make_float2(ref[nb][j], l);
-#pragma unroll
-        for (int i = 0; i < S::kMb; ++i) {
-          const int lo = F8 ? 16 * c + 2 * i : D == 128 ? 8 * c + i : 8 * c + 2 * i;
-          const int hi = !F8 && D == 128 ? 64 + lo : lo + 1;
-          sh_o[warp][g * kStride + lo] = o[nb][i][j];
-          sh_o[warp][g * kStride + hi] = o[nb][i][j + 2];
-        }
-      }
+    tok_put<D, F8, NB>(ref, sum, o, sh_ml[warp], sh_o[warp]);
     __syncthreads();
     const bool begins = tile_end == seg, whole = begins && tile_end == nt;
     const int slot = 2 * (int)blockIdx.x + (begins ? 1 : 0);
@@ -494,6 +521,84 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
       if (nt == 0) break;
     }
   }
+}
+
+// ---------------------------------------------------------------- few rows
+// The keys of a row in one cluster, whose warps take them in turn: with few rows and short caches the pieces meet in distributed
+// shared memory, and neither a deal nor a second launch is needed.
+template <int NB> constexpr int kFewWarps = NB == 1 ? 6 : 4;
+template <int D, bool F8, int NB>
+__global__ void __launch_bounds__(kFewWarps<NB> * 32, 2) token_few_kernel(const TokenParams p) {
+  namespace cg = cooperative_groups;
+  using S = TokShape<D, F8>;
+  constexpr int HB = 8 * NB, kWarps = kFewWarps<NB>, kThreads = kWarps * 32, kMaxCluster = 16;
+  __shared__ float sh_o[kWarps][HB * (D + 1)];
+  __shared__ float2 sh_ml[kWarps][HB];
+  __shared__ float part_o[HB * D];               // of this CTA
+  __shared__ float2 part_ml[HB];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int cl = (int)cluster.num_blocks(), me = (int)cluster.block_rank();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  pdl_wait();
+  const int line = blockIdx.x / cl, r = line / p.n_kv_heads, h = line % p.n_kv_heads, heads = p.group;       // (one block of heads)
+  const int len = __ldcg(p.kv_len + r);
+  bf16* out = p.out + (size_t)line * heads * D;
+  // (the CTAs of a cluster leave together here or meet at the barriers below)
+  if (len < 0) return;
+  if (len > (long long)p.max_pages_per_req * kPage) {
+    if (me == 0 && h == 0 && tid == 0) atomicOr(p.status, FB_ST_BAD_STATE);
+    return;
+  }
+  if (len == 0) {
+    if (me == 0)
+      for (int i = tid; i < heads * (D / 8); i += kThreads) reinterpret_cast<uint4*>(out)[i] = make_uint4(0, 0, 0, 0);
+    return;
+  }
+  float ref[NB][2], sum[NB][2], o[NB][S::kMb][4];
+  const int first = (me * kWarps + warp) * S::kKeys, step = cl * kWarps * S::kKeys, steps = len > first ? (len - first + step - 1) / step : 0;
+  tok_stream<D, F8, NB, false, 0>(p, r, h, 0, len, first, steps, step, ref, sum, o);
+  tok_put<D, F8, NB>(ref, sum, o, sh_ml[warp], sh_o[warp]);
+  __syncthreads();
+  for (int i = tid; i < heads * D; i += kThreads) {
+    const int g = i / D, d = i % D;
+    float m = sh_ml[0][g].x;
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sh_ml[w][g].x);
+    float l = 0.f, x = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const float f = ex2(sh_ml[w][g].x - m);
+      l += sh_ml[w][g].y * f;
+      x += sh_o[w][g * (D + 1) + d] * f;
+    }
+    part_o[i] = x;
+    if (d == 0) part_ml[g] = make_float2(m, l);
+  }
+  if (cl > 1) cluster.sync();
+  else __syncthreads();
+  // the CTAs' pieces in order; a CTA forms its share of the outputs
+  const float vs = F8 ? p.v_scale[h] : 1.f;
+  const int share = (heads * D + cl - 1) / cl;
+  for (int i = me * share + tid; i < min(heads * D, (me + 1) * share); i += kThreads) {
+    float2 ml[kMaxCluster];
+    float v[kMaxCluster], m = kNoRef, l = 0.f, x = 0.f;
+#pragma unroll
+    for (int q = 0; q < kMaxCluster; ++q)
+      if (q < cl) {
+        ml[q] = cl > 1 ? *cluster.map_shared_rank(&part_ml[i / D], q) : part_ml[i / D];
+        v[q] = cl > 1 ? *cluster.map_shared_rank(&part_o[i], q) : part_o[i];
+        m = fmaxf(m, ml[q].x);
+      }
+#pragma unroll
+    for (int q = 0; q < kMaxCluster; ++q)
+      if (q < cl) {
+        const float f = ex2(ml[q].x - m);
+        l += ml[q].y * f;
+        x += v[q] * f;
+      }
+    out[i] = __float2bfloat16_rn(l == 0.f ? 0.f : x / l * vs);
+  }
+  if (cl > 1) cluster.sync();                    // (no CTA leaves while another may read its piece)
 }
 
 // ---------------------------------------------------------------- the join
@@ -668,9 +773,33 @@ static TokWs tok_ws(const fb_ctx* ctx, bool weights) {
 }
 size_t token_workspace_bytes(const fb_ctx* ctx, bool weights) { return tok_ws(ctx, weights).total; }
 
+// CTAs of a cluster that takes a row (0: the rows are dealt): as many as two an SM allow, at most sixteen, and no more than
+// the capacity has work for.
+static int tok_cluster(const fb_ctx* ctx, int block_heads, int keys) {
+  const fb_config& c = ctx->cfg;
+  const long long rows = (long long)c.max_requests * c.n_kv_heads, cap = (long long)c.max_pages_per_req * kPage;
+  if (ctx->group > block_heads || cap > kFewCapacity || rows > kFewRows) return 0;
+  int cl = 16;
+  while (cl > 1 && (rows * cl > 2 * kSms || cl / 2 * keys >= cap)) cl /= 2;
+  return cl;
+}
+
 template <int D, bool F8, int NB, bool W>
 static int launch_token(fb_ctx* ctx, const TokenParams& p, cudaStream_t stream) {
   const fb_config& c = ctx->cfg;
+  if constexpr (!W) {
+    if (const int cl = tok_cluster(ctx, 8 * NB, kFewWarps<NB> * TokShape<D, F8>::kKeys)) {
+      const auto kernel = token_few_kernel<D, F8, NB>;
+      int dev = 0;
+      if (int e = cuda_err(ctx, cudaGetDevice(&dev), "cudaGetDevice")) return e;
+      if (cl > 8 && ctx->token_device != dev) {       // (sixteen have to be asked for; the context remembers where it has)
+        if (int e = cuda_err(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1), "cluster attr")) return e;
+        ctx->token_device = dev;
+      }
+      return cuda_err(ctx, launch_pdl_cluster(kernel, (unsigned)(c.max_requests * c.n_kv_heads * cl), kFewWarps<NB> * 32, 0, stream, cl, p),
+                      "token_few_kernel launch");
+    }
+  }
   if (int e = cuda_err(ctx, launch_pdl(token_attn_kernel<D, F8, NB, W>, p.n_ctas, kTokThreads, 0, stream, p), "token_attn_kernel launch"))
     return e;
   const long long pairs = (long long)c.max_requests * c.n_kv_heads, step = kWeightAt * kTokThreads;

@@ -94,8 +94,11 @@ def test_lengths_and_head_layouts(heads, fp8):
     np.testing.assert_array_equal(weight, case.kv_weight)
     got2, weight, status = attend(case, accumulate=True, garbage=0)
     assert status == 0
-    np.testing.assert_array_equal(bits(got), bits(got2))
+    check_out(case, got2, ref, a)                     # (short caches in few rows: the two forms add the keys in other orders)
     check_weights(case, weight, w)
+    again = [attend(case, accumulate=acc)[0] for acc in (False, True)]
+    np.testing.assert_array_equal(bits(again[0]), bits(got))
+    np.testing.assert_array_equal(bits(again[1]), bits(got2))
 
 
 @pytest.mark.parametrize("lens,heads,fp8", [
@@ -109,6 +112,31 @@ def test_long_and_ragged_batches(lens, heads, fp8):
     assert status == 0
     check_out(case, got, ref, a)
     check_weights(case, weight, w)
+
+
+@pytest.mark.parametrize("heads,fp8", [((32, 8, 128), False), ((32, 8, 128), True), ((4, 1, 64), False), ((16, 1, 128), False),
+                                       ((32, 32, 128), False), ((16, 1, 128), True)])
+@pytest.mark.parametrize("n", [1, 15, 16, 33, 95, 96, 97, 191, 193, 1000, 1536, 1537, 3001, 4031, 4096, 4097])
+def test_one_request_around_the_steps_of_a_cluster(heads, fp8, n):
+    """Short caches in few rows take a cluster of up to sixteen CTAs each, longer ones (the last) are dealt."""
+    case = Case([n], heads, fp8, seed=n)
+    ref, a, _ = reference(case)
+    got, _, status = attend(case)
+    assert status == 0
+    check_out(case, got, ref, a)
+
+
+def test_few_rows_with_room_to_spare():
+    """Capacity far above the lengths, a page that is no page behind them, ragged rows, two calls in a row."""
+    case = Case([3, 0, -1, 700, 64, 1], (8, 2, 128), seed=21, pages_per_req=40)
+    case.page_table[0, 1:] = -1
+    case.page_table[3, 11:] = 1 << 30
+    ref, a, _ = reference(case)
+    ctx = case.context()
+    for _ in range(2):
+        got, _, status = attend(case, ctx=ctx)
+        assert status == 0
+        check_out(case, got, ref, a)
 
 
 @pytest.mark.parametrize("shape", ["rising", "falling", "dominant", "equal", "far"])
@@ -207,18 +235,19 @@ def test_softmax_scale_of_the_context():
 
 
 @pytest.mark.parametrize("fp8", [False, True])
-def test_a_captured_call_follows_lengths_pages_and_queries(fp8):
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_a_captured_call_follows_lengths_pages_and_queries(fp8, accumulate):
     case = Case([300, 900, 64, 0], (16, 4, 128), fp8, seed=10)
     ctx = case.context()
     cache, kp, vp = case.device()
     q, status = case.q.to(DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
     out, ws = torch.zeros_like(q), B.alloc_token_workspace(ctx, DEV, True)
-    call(case, ctx, cache, q, kp, vp, out, ws, status, True)
+    call(case, ctx, cache, q, kp, vp, out, ws, status, accumulate)
     torch.cuda.synchronize()
     s = torch.cuda.Stream()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=s):
-        call(case, ctx, cache, q, kp, vp, out, ws, status, True)
+        call(case, ctx, cache, q, kp, vp, out, ws, status, accumulate)
     rng = np.random.default_rng(3)
     for lens in ([300, 900, 64, 0], [1, 65, -1, 899], [0, 0, 0, 0], [120, 1, 500, 2]):
         cache.kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
@@ -237,7 +266,7 @@ def test_a_captured_call_follows_lengths_pages_and_queries(fp8):
         o1, w1 = out.clone(), cache.kv_weight.clone()
         cache.kv_weight.zero_()
         out.fill_(SENTINEL)
-        call(case, ctx, cache, q, kp, vp, out, ws, status, True)
+        call(case, ctx, cache, q, kp, vp, out, ws, status, accumulate)
         torch.cuda.synchronize()
         assert torch.equal(o1, out) and torch.equal(w1, cache.kv_weight)
     assert int(status) == 0
