@@ -558,6 +558,7 @@ __global__ void __launch_bounds__(kFewWarps<NB> * 32, 2) token_few_kernel(const 
   const int first = (me * kWarps + warp) * S::kKeys, step = cl * kWarps * S::kKeys, steps = len > first ? (len - first + step - 1) / step : 0;
   tok_stream<D, F8, NB, false, 0>(p, r, h, 0, len, first, steps, step, ref, sum, o);
   tok_put<D, F8, NB>(ref, sum, o, sh_ml[warp], sh_o[warp]);
+  const float vs = F8 ? p.v_scale[h] : 1.f;
   __syncthreads();
   for (int i = tid; i < heads * D; i += kThreads) {
     const int g = i / D, d = i % D;
@@ -571,13 +572,13 @@ __global__ void __launch_bounds__(kFewWarps<NB> * 32, 2) token_few_kernel(const 
       l += sh_ml[w][g].y * f;
       x += sh_o[w][g * (D + 1) + d] * f;
     }
+    if (cl == 1) { out[i] = __float2bfloat16_rn(l == 0.f ? 0.f : x / l * vs); continue; }
     part_o[i] = x;
     if (d == 0) part_ml[g] = make_float2(m, l);
   }
-  if (cl > 1) cluster.sync();
-  else __syncthreads();
+  if (cl == 1) return;
+  cluster.sync();
   // the CTAs' pieces in order; a CTA forms its share of the outputs
-  const float vs = F8 ? p.v_scale[h] : 1.f;
   const int share = (heads * D + cl - 1) / cl;
   for (int i = me * share + tid; i < min(heads * D, (me + 1) * share); i += kThreads) {
     float2 ml[kMaxCluster];
@@ -585,8 +586,8 @@ __global__ void __launch_bounds__(kFewWarps<NB> * 32, 2) token_few_kernel(const 
 #pragma unroll
     for (int q = 0; q < kMaxCluster; ++q)
       if (q < cl) {
-        ml[q] = cl > 1 ? *cluster.map_shared_rank(&part_ml[i / D], q) : part_ml[i / D];
-        v[q] = cl > 1 ? *cluster.map_shared_rank(&part_o[i], q) : part_o[i];
+        ml[q] = *cluster.map_shared_rank(&part_ml[i / D], q);
+        v[q] = *cluster.map_shared_rank(&part_o[i], q);
         m = fmaxf(m, ml[q].x);
       }
 #pragma unroll
@@ -598,7 +599,7 @@ __global__ void __launch_bounds__(kFewWarps<NB> * 32, 2) token_few_kernel(const 
       }
     out[i] = __float2bfloat16_rn(l == 0.f ? 0.f : x / l * vs);
   }
-  if (cl > 1) cluster.sync();                    // (no CTA leaves while another may read its piece)
+  cluster.sync();                                // (no CTA leaves while another may read its piece)
 }
 
 // ---------------------------------------------------------------- the join
