@@ -39,6 +39,7 @@ template <bool F8> constexpr float kTokShift = F8 ? 7.f : 0.f;
 
 using bf16 = __nv_bfloat16;
 
+struct TokPieces;
 struct TokenParams {
   const int32_t *kv_len, *page_table;
   float* kv_weight;
@@ -49,6 +50,7 @@ struct TokenParams {
   int32_t* status;
   float* part_o;                         // [2 n_ctas][heads of a block][d] unnormalised outputs of the pieces
   float2* part_ml;                       // [2 n_ctas][heads of a block] reference (log2), sum
+  TokPieces* row_pieces;                 // [rows] (more than kDealAgain requests)
   float2* row_ml;                        // [rows][heads of a block] reference and sum of rows that were not cut (weights only)
   float* scores;                         // [requests][KV heads][capacity][group] (log2; weights only)
   int32_t requests, group, n_kv_heads, head_blocks, max_pages_per_req, num_pages, n_ctas, join_ctas;
@@ -122,7 +124,7 @@ __device__ __forceinline__ TokDeal tok_deal(const TokenParams& p, int tile, int 
   const int lane = threadIdx.x & 31, rows = p.n_kv_heads * p.head_blocks;
   int longest = tok_tiles(p, len, tile);
   long long all = longest, before = lane < upto ? longest : 0;
-#pragma unroll 4
+#pragma unroll 8
   for (int r = 32 + lane; r < p.requests; r += 32) {
     const int n = tok_tiles(p, __ldcg(p.kv_len + r), tile);
     all += n;
@@ -138,19 +140,24 @@ __device__ __forceinline__ TokDeal tok_deal(const TokenParams& p, int tile, int 
   TokDeal d;
   d.total = all * rows;
   d.before = before * rows;
-  d.share = max(tok_div(d.total + p.n_ctas - 1, p.n_ctas), (long long)((longest + kMostPieces - 1) / kMostPieces));
+  d.share = max(max(tok_div(d.total + p.n_ctas - 1, p.n_ctas), (long long)((longest + kMostPieces - 1) / kMostPieces)), 1ll);
   return d;
 }
-// The pieces of a row: CTAs c0.. of the deal; a piece lies in slot 2 c + 1 where the row starts in that CTA, else in 2 c.
-struct TokPieces {
-  long long start, share;
+// The pieces of a row: of CTAs c0, c0 + 1, ...  The first lies in the odd slot of its CTA (the row starts in it), the others in the
+// even ones.
+struct __align__(8) TokPieces {
   int c0, n;
-  __device__ __forceinline__ TokPieces(long long start_, int nt, long long share_) : start(start_), share(share_) {
-    c0 = (int)tok_div(start, share);
-    n = (int)tok_div(start + nt - 1, share) - c0 + 1;
-  }
-  __device__ __forceinline__ int slot(int i) const { return 2 * (c0 + i) + ((c0 + i) * share <= start ? 1 : 0); }
+  __device__ __forceinline__ int slot(int i) const { return 2 * (c0 + i) + (i == 0 ? 1 : 0); }
 };
+__device__ __forceinline__ TokPieces tok_pieces(long long start, int nt, long long share) {
+  TokPieces k;
+  k.c0 = (int)tok_div(start, share);
+  k.n = (int)tok_div(start + nt - 1, share) - k.c0 + 1;
+  return k;
+}
+// Up to as many requests the join finds the pieces from the lengths, while the stream still runs; for more the stream leaves
+// them per row, since a look at all lengths by every CTA of the join takes longer than one read more behind the stream.
+constexpr int kDealAgain = 32;
 
 // ---------------------------------------------------------------- the stream
 // A warp's share of the keys of query heads [hb * 8 NB, ...) of (request r, KV head h): `steps` steps of S::kKeys keys from key
@@ -444,6 +451,7 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
   constexpr int HB = 8 * NB, kStride = D + 1;
   __shared__ float sh_o[kTokWarps][HB * kStride];
   __shared__ float2 sh_ml[kTokWarps][HB];
+  __shared__ int sh_share;
   pdl_wait_then_release();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rows = p.n_kv_heads * p.head_blocks;
@@ -452,27 +460,33 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
   long long at = (long long)blockIdx.x * deal.share;
   int left = (int)min(deal.share, deal.total - at > 0 ? deal.total - at : 0);
   if (left <= 0) return;
-  // the request that holds tile `at`, its length and tiles
+  if (tid == 0) sh_share = (int)min(deal.share, 0x7fffffffll);       // (read behind the barrier at the end of a segment)
+  // the request that holds tile `at`, its length and tiles; 128 lengths under way at a time
   int r = 0, nt = 0;
-  for (int r0 = 0; r0 < p.requests; r0 += 32) {
-    if (r0 > 0) len = tok_len(p, r0 + lane);
-    const int n = tok_tiles(p, len, S::kTile);
-    int incl = n;
+  for (int r0 = 0; r0 < p.requests && nt == 0; r0 += 128) {
+    int lens[4];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += v;
+    for (int u = 0; u < 4; ++u) lens[u] = r0 + u == 0 ? len : r0 + 32 * u < p.requests ? tok_len(p, r0 + 32 * u + lane) : 0;
+#pragma unroll 1
+    for (int u = 0; u < 4 && nt == 0; ++u) {
+      const int mine = u == 0 ? lens[0] : u == 1 ? lens[1] : u == 2 ? lens[2] : lens[3], n = tok_tiles(p, mine, S::kTile);
+      int incl = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      const unsigned here = __ballot_sync(0xffffffffu, at < (long long)incl * rows);
+      if (here) {
+        const int l = __ffs(here) - 1;
+        nt = __shfl_sync(0xffffffffu, n, l);
+        len = __shfl_sync(0xffffffffu, mine, l);
+        at -= (long long)(__shfl_sync(0xffffffffu, incl, l) - nt) * rows;
+        r = r0 + 32 * u + l;
+      } else {
+        at -= (long long)__shfl_sync(0xffffffffu, incl, 31) * rows;
+      }
     }
-    const unsigned here = __ballot_sync(0xffffffffu, at < (long long)incl * rows);
-    if (here) {
-      const int l = __ffs(here) - 1;
-      nt = __shfl_sync(0xffffffffu, n, l);
-      len = __shfl_sync(0xffffffffu, len, l);
-      at -= (long long)(__shfl_sync(0xffffffffu, incl, l) - nt) * rows;
-      r = r0 + l;
-      break;
-    }
-    at -= (long long)__shfl_sync(0xffffffffu, incl, 31) * rows;
   }
   if (nt == 0) return;                         // (not reached while nobody writes the lengths)
   int row = (int)tok_div(at, nt), tile = (int)(at - (long long)row * nt);
@@ -491,6 +505,10 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
     const float vs = F8 ? p.v_scale[h] : 1.f;
     bf16* out = p.out + (((size_t)r * p.n_kv_heads + h) * p.group + hb * HB) * D;
     const int heads = min(HB, p.group - hb * HB);
+    if (begins && tid == 0 && p.requests > kDealAgain) {
+      const int rest = nt - seg;                 // of the row, to the CTAs behind this one
+      p.row_pieces[(size_t)r * rows + row] = TokPieces{(int)blockIdx.x, 1 + rest / sh_share + (rest % sh_share ? 1 : 0)};
+    }
     for (int i = tid; i < heads * D; i += kTokThreads) {
       const int g = i / D, d = i % D;
       float m = sh_ml[0][g].x;
@@ -659,7 +677,8 @@ __global__ void __launch_bounds__(kTokThreads) token_join_kernel(const TokenPara
   // (the kernel behind this one waits for this one alone: one CTA at least has to have waited for the stream)
   const bool keeper = blockIdx.x == 0 && blockIdx.y == 0;
   // (the lengths are older than the stream kernel, which waited itself before it let this one start)
-  const int first = tok_len(p, lane), len = tok_len(p, r), nt = tok_tiles(p, len, S::kTile);
+  const bool again = p.requests <= kDealAgain;
+  const int first = again ? tok_len(p, lane) : 0, len = tok_len(p, r), nt = tok_tiles(p, len, S::kTile);
   const bool idle = nt == 0 || (weights && hb != 0);
   if (!weights && nt == 0 && blockIdx.y == 0) {  // zeros where nothing is stored, a report where the length is no length
     if (len > 0 && row == 0 && tid == 0) atomicOr(p.status, FB_ST_BAD_STATE);
@@ -671,64 +690,72 @@ __global__ void __launch_bounds__(kTokThreads) token_join_kernel(const TokenPara
     }
   }
   if (idle && !keeper) return;
-  const TokDeal deal = tok_deal(p, S::kTile, first, r);
-  const TokPieces k(deal.before + (long long)row * nt, nt, deal.share);
-  if (keeper || weights || k.n > 1) pdl_wait_only();
+  TokDeal deal{};
+  if (again && nt > 0) deal = tok_deal(p, S::kTile, first, r);
+  auto pieces_of = [&](int of) {
+    if (again) return tok_pieces(deal.before + (long long)of * nt, nt, deal.share);
+    const int2 v = __ldcg(reinterpret_cast<const int2*>(p.row_pieces) + (size_t)r * rows + of);
+    return TokPieces{v.x, v.y};
+  };
+  TokPieces k{0, 1};
+  if (again && nt > 0) k = pieces_of(row);
+  if (keeper || weights || !again || k.n > 1) pdl_wait_only();
   if (idle) return;
+  if (!again) k = pieces_of(row);
   if (!weights) {
     if (k.n == 1) return;
     for (int g = blockIdx.y; g < min(HB, p.group - hb * HB); g += p.join_ctas) {
-    const int grp = tid / kLanes, d4 = tid % kLanes;
-    const float vs = F8 ? p.v_scale[h] : 1.f;
-    // the outputs of the first pieces are under way while references and sums are put together
-    auto piece = [&](int i) { return __ldcg(reinterpret_cast<const float4*>(p.part_o + ((size_t)k.slot(i) * HB + g) * D) + d4); };
-    float4 v[kAhead];
+      const int grp = tid / kLanes, d4 = tid % kLanes;
+      const float vs = F8 ? p.v_scale[h] : 1.f;
+      // the outputs of the first pieces are under way while references and sums are put together
+      auto piece = [&](int i) { return __ldcg(reinterpret_cast<const float4*>(p.part_o + ((size_t)k.slot(i) * HB + g) * D) + d4); };
+      float4 v[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) v[u] = grp + u * kGroups < k.n ? piece(grp + u * kGroups) : make_float4(0.f, 0.f, 0.f, 0.f);
-    float m = kNoRef;
-    for (int i = tid; i < k.n; i += kTokThreads) {
-      const float2 x = __ldcg(p.part_ml + (size_t)k.slot(i) * HB + g);
-      ml[i] = x;
-      m = fmaxf(m, x.x);
-    }
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-    if (lane == 0) tops[warp] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i0 = grp; i0 < k.n; i0 += kAhead * kGroups) {
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int i = i0 + u * kGroups, next = i + kAhead * kGroups;
-        if (i < k.n) {
-          const float f = ex2(ml[i].x - m);
-          acc.x += v[u].x * f; acc.y += v[u].y * f; acc.z += v[u].z * f; acc.w += v[u].w * f;
-        }
-        if (next < k.n) v[u] = piece(next);
+      for (int u = 0; u < kAhead; ++u) v[u] = grp + u * kGroups < k.n ? piece(grp + u * kGroups) : make_float4(0.f, 0.f, 0.f, 0.f);
+      float m = kNoRef;
+      for (int i = tid; i < k.n; i += kTokThreads) {
+        const float2 x = __ldcg(p.part_ml + (size_t)k.slot(i) * HB + g);
+        ml[i] = x;
+        m = fmaxf(m, x.x);
       }
-    }
-    float l = 0.f;
-    for (int i = tid; i < k.n; i += kTokThreads) l += ml[i].y * ex2(ml[i].x - m);
 #pragma unroll
-    for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-    if (lane == 0) sums[warp] = l;
-    red[tid] = acc;
-    __syncthreads();
-    if (tid < D) {
-      float x = 0.f;
+      for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+      if (lane == 0) tops[warp] = m;
+      __syncthreads();
+      m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i0 = grp; i0 < k.n; i0 += kAhead * kGroups) {
 #pragma unroll
-      for (int w = 0; w < kGroups; ++w) x += reinterpret_cast<const float*>(red)[w * D + tid];
-      const float s = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-      p.out[(((size_t)r * p.n_kv_heads + h) * p.group + hb * HB + g) * D + tid] = __float2bfloat16_rn(s == 0.f ? 0.f : x / s * vs);
-    }
-    __syncthreads();
+        for (int u = 0; u < kAhead; ++u) {
+          const int i = i0 + u * kGroups, next = i + kAhead * kGroups;
+          if (i < k.n) {
+            const float f = ex2(ml[i].x - m);
+            acc.x += v[u].x * f; acc.y += v[u].y * f; acc.z += v[u].z * f; acc.w += v[u].w * f;
+          }
+          if (next < k.n) v[u] = piece(next);
+        }
+      }
+      float l = 0.f;
+      for (int i = tid; i < k.n; i += kTokThreads) l += ml[i].y * ex2(ml[i].x - m);
+#pragma unroll
+      for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+      if (lane == 0) sums[warp] = l;
+      red[tid] = acc;
+      __syncthreads();
+      if (tid < D) {
+        float x = 0.f;
+#pragma unroll
+        for (int w = 0; w < kGroups; ++w) x += reinterpret_cast<const float*>(red)[w * D + tid];
+        const float s = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+        p.out[(((size_t)r * p.n_kv_heads + h) * p.group + hb * HB + g) * D + tid] = __float2bfloat16_rn(s == 0.f ? 0.f : x / s * vs);
+      }
+      __syncthreads();
     }
   } else if constexpr (W) {
     __shared__ float2 top[kTileM];               // reference, 1 / sum (a group has at most 128 heads)
     for (int g = warp; g < p.group; g += kTokWarps) {
       const int b = g / HB, gl = g % HB;
-      const TokPieces q(deal.before + (long long)(row + b) * nt, nt, deal.share);
+      const TokPieces q = pieces_of(row + b);
       float m = kNoRef, l = 0.f;
       if (q.n == 1) {
         const float2 v = __ldcg(p.row_ml + ((size_t)r * rows + row + b) * HB + gl);
@@ -758,7 +785,7 @@ __global__ void __launch_bounds__(kTokThreads) token_join_kernel(const TokenPara
 static int tok_heads(const fb_ctx* ctx) { return ctx->group > 8 ? 16 : 8; }
 static int tok_ctas(const fb_ctx* ctx) { return (ctx->group > 8 ? 2 : kTokCtasPerSm) * kSms; }
 
-struct TokWs { size_t part_ml, part_o, row_ml, scores, total; };
+struct TokWs { size_t part_ml, part_o, row_pieces, row_ml, scores, total; };
 static TokWs tok_ws(const fb_ctx* ctx, bool weights) {
   const fb_config& c = ctx->cfg;
   const size_t hb = tok_heads(ctx), rows = (size_t)c.max_requests * c.n_kv_heads * ((ctx->group + hb - 1) / hb);
@@ -767,7 +794,8 @@ static TokWs tok_ws(const fb_ctx* ctx, bool weights) {
   TokWs w;
   w.part_ml = 0;
   w.part_o = w.part_ml + up(slots * hb * sizeof(float2));
-  w.row_ml = w.part_o + up(slots * hb * c.head_dim * sizeof(float));
+  w.row_pieces = w.part_o + up(slots * hb * c.head_dim * sizeof(float));
+  w.row_ml = w.row_pieces + (c.max_requests > kDealAgain ? up(rows * sizeof(TokPieces)) : 0);
   w.scores = w.row_ml + (weights ? up(rows * hb * sizeof(float2)) : 0);
   w.total = w.scores + (weights ? up((size_t)c.max_requests * c.n_q_heads * c.max_pages_per_req * kPage * sizeof(float)) : 0);
   return w;
@@ -832,6 +860,7 @@ int launch_token_attn(fb_ctx* ctx, const fb_cache* kv, const void* q, const void
   p.k_scale = k_scale; p.v_scale = v_scale; p.out = static_cast<bf16*>(out); p.status = status;
   p.part_ml = reinterpret_cast<float2*>(base + w.part_ml);
   p.part_o = reinterpret_cast<float*>(base + w.part_o);
+  p.row_pieces = reinterpret_cast<TokPieces*>(base + w.row_pieces);
   p.row_ml = reinterpret_cast<float2*>(base + w.row_ml);
   p.scores = reinterpret_cast<float*>(base + w.scores);
   p.requests = c.max_requests; p.group = ctx->group; p.n_kv_heads = c.n_kv_heads;

@@ -126,6 +126,23 @@ def test_one_request_around_the_steps_of_a_cluster(heads, fp8, n):
     check_out(case, got, ref, a)
 
 
+@pytest.mark.parametrize("heads,fp8,n", [((8, 2, 128), False, 33), ((4, 1, 64), False, 300), ((8, 2, 128), True, 129), ((64, 2, 128), False, 40),
+                                         ((16, 1, 128), False, 513)])
+def test_many_requests(heads, fp8, n):
+    """More requests than the deal looks at at once; some have nothing, some are none, one is long."""
+    rng = np.random.default_rng(n)
+    lens = rng.integers(-1, 150, n)
+    lens[rng.random(n) < 0.2] = 0
+    lens[n // 2] = 2000
+    case = Case(lens, heads, fp8, seed=22)
+    ref, a, w = reference(case)
+    for acc in (False, True):
+        got, weight, status = attend(case, accumulate=acc)
+        assert status == 0
+        check_out(case, got, ref, a)
+    check_weights(case, weight, w)
+
+
 def test_few_rows_with_room_to_spare():
     """Capacity far above the lengths, a page that is no page behind them, ragged rows, two calls in a row."""
     case = Case([3, 0, -1, 700, 64, 1], (8, 2, 128), seed=21, pages_per_req=40)
