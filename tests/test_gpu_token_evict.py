@@ -271,6 +271,55 @@ def test_steps_of_append_attend_evict(heads, fp8):
     assert list(lens) == [80, 31, 80]
 
 
+@pytest.mark.parametrize("heads,fp8,accumulate,pages", [((8, 2, 128), False, True, 4), ((32, 8, 128), True, True, 4), ((32, 8, 128), False, False, 4),
+                                                        ((8, 2, 128), False, False, 40)])
+def test_a_captured_step_replayed_as_the_lengths_grow(heads, fp8, accumulate, pages):
+    """Lengths advanced, token stored, attended to and the caches cut, captured as the context's first calls and
+    replayed, against the same calls made directly."""
+    case = aged(Case([70, 0, 130, -1], heads, fp8, seed=15, pages_per_req=pages), seed=16)
+    case.kv_weight[:] = case.rng.random(case.kv_weight.shape)
+    sides = []
+    for _ in range(2):
+        ctx = case.context()
+        cache, kp, vp = case.device()
+        R, hkv, hq, d = case.R, case.hkv, case.hq, case.d
+        io = [torch.zeros(R, n, d, dtype=torch.bfloat16, device=DEV) for n in (hkv, hkv, hq)]
+        out, status = torch.zeros(R, hq, d, dtype=torch.bfloat16, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+        keep = torch.full((R,), 100, dtype=torch.int32, device=DEV)
+        ws, wse = B.alloc_token_workspace(ctx, DEV, accumulate), B.alloc_evict_workspace(ctx, DEV)
+        live = torch.tensor([1, 1, 1, 0], dtype=torch.int32, device=DEV)
+        sc = case.dev_scales() if fp8 else []
+
+        def step(ctx=ctx, cache=cache, kp=kp, vp=vp, io=io, out=out, status=status, keep=keep, ws=ws, wse=wse, live=live, sc=sc):
+            cache.kv_len.add_(live)
+            cache.tok_pos.add_(live)
+            append, attn = (B.fb_append_kv_fp8, B.fb_token_attn_fp8) if fp8 else (B.fb_append_kv, B.fb_token_attn)
+            append(ctx, cache, io[0], io[1], kp, vp, *sc, status, 10000.0)
+            attn(ctx, cache, io[2], kp, vp, *sc, out, ws, status, accumulate)
+            B.fb_evict_kv(ctx, cache, keep, 8, 2, kp, vp, wse, status)
+        sides.append((step, io, out, cache, kp, vp, status))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        sides[0][0]()
+    gen = torch.Generator().manual_seed(1)
+    for _ in range(25):
+        new = [torch.randn(x.shape, generator=gen).to(torch.bfloat16) for x in sides[0][1]]
+        for _, io, *_ in sides:
+            for x, y in zip(io, new):
+                x.copy_(y)
+        graph.replay()
+        sides[1][0]()
+        torch.cuda.synchronize()
+        (_, _, o0, c0, k0, v0, s0), (_, _, o1, c1, k1, v1, s1) = sides
+        assert int(s0) == int(s1) == 0
+        for a, b in ((c0.kv_len, c1.kv_len), (c0.kv_pos, c1.kv_pos), (c0.kv_weight, c1.kv_weight), (o0, o1)):
+            assert torch.equal(a, b)
+        np.testing.assert_array_equal(bits(k0), bits(k1))
+        np.testing.assert_array_equal(bits(v0), bits(v1))
+    assert c0.kv_len.tolist() == [95, 25, 100, -1]
+
+
 def test_block_decoding_goes_on_over_a_cut_prefix():
     """A prefix weighed by one query, cut, and read by the block attention: prefix_len is the cut length, and the block
     attends to what stays."""
