@@ -122,19 +122,27 @@ constexpr int kMostPieces = 64;
 struct TokDeal { long long total, before, share; };
 __device__ __forceinline__ TokDeal tok_deal(const TokenParams& p, int tile, int len, int upto) {
   const int lane = threadIdx.x & 31, rows = p.n_kv_heads * p.head_blocks;
-  int longest = tok_tiles(p, len, tile);
-  long long all = longest, before = lane < upto ? longest : 0;
+  const int n0 = tok_tiles(p, len, tile);
+  int longest = n0;
+  long long all, before;
+  if (p.requests <= 32) {                        // (32 counts below 2^25 each)
+    all = __reduce_add_sync(0xffffffffu, n0);
+    before = __reduce_add_sync(0xffffffffu, lane < upto ? n0 : 0);
+  } else {
+    all = n0;
+    before = lane < upto ? n0 : 0;
 #pragma unroll 8
-  for (int r = 32 + lane; r < p.requests; r += 32) {
-    const int n = tok_tiles(p, __ldcg(p.kv_len + r), tile);
-    all += n;
-    before += r < upto ? n : 0;
-    longest = max(longest, n);
-  }
+    for (int r = 32 + lane; r < p.requests; r += 32) {
+      const int n = tok_tiles(p, __ldcg(p.kv_len + r), tile);
+      all += n;
+      before += r < upto ? n : 0;
+      longest = max(longest, n);
+    }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    all += __shfl_xor_sync(0xffffffffu, all, o);
-    before += __shfl_xor_sync(0xffffffffu, before, o);
+    for (int o = 16; o > 0; o >>= 1) {
+      all += __shfl_xor_sync(0xffffffffu, all, o);
+      before += __shfl_xor_sync(0xffffffffu, before, o);
+    }
   }
   longest = __reduce_max_sync(0xffffffffu, longest);
   TokDeal d;
@@ -463,6 +471,10 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
   if (tid == 0) sh_share = (int)min(deal.share, 0x7fffffffll);       // (read behind the barrier at the end of a segment)
   // the request that holds tile `at`, its length and tiles; 128 lengths under way at a time
   int r = 0, nt = 0;
+  if (p.requests == 1) {
+    len = __shfl_sync(0xffffffffu, len, 0);
+    nt = tok_tiles(p, len, S::kTile);
+  }
   for (int r0 = 0; r0 < p.requests && nt == 0; r0 += 128) {
     int lens[4];
 #pragma unroll
