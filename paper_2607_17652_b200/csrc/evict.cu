@@ -8,7 +8,7 @@
 // Kernel 1, a cluster of 1 to 8 CTAs per (request, KV head): the rank of the last key that stays, by counting.  The range
 // of the ranks is cut into 512 bins, the bin that holds the boundary into 512 again, until all keys of a bin stay
 // (two or three times, 512 bins that follow the range spread the counts over many addresses); then the lists of freed
-// places and of keys to move, both in index order by ballots and one scan.  Bound by its chain of block-wide steps: loops
+// places and of keys to move, both in index order by the threads' own counts and one scan.  Bound by its chain of block-wide steps: loops
 // are kept short, since every CTA runs the code once, and what goes between the CTAs of a cluster is kept small (one request
 // of 28,123 keys: digits of 11 bits and code unrolled over keys in registers 28 us, this form 16).  Reads 8 bytes a stored key.
 // Kernel 2: the rows of K and V, the weights and the positions, eight rows a warp under way.
@@ -23,8 +23,7 @@ namespace fb {
 namespace cg = cooperative_groups;
 
 constexpr int kSelThreads = 256, kSelWarps = kSelThreads / 32;
-constexpr int kSelPer = 32;                       // keys of a thread
-constexpr int kSelCap = kSelThreads * kSelPer;    // ... of a CTA, in shared memory
+constexpr int kSelCap = 8192;                     // keys of a CTA, in shared memory
 constexpr int kBinBits = 9, kBins = 1 << kBinBits, kMaxCluster = 8;
 constexpr int kMoveThreads = 256, kMoveWarps = kMoveThreads / 32, kMoveAhead = 8;
 
@@ -49,30 +48,27 @@ __device__ __forceinline__ uint32_t rank_of(float w, int pos, const Guarded& g) 
   return pos < g.sinks || (g.any && pos >= g.first) ? 0xffffffffu : k;
 }
 
-// Exclusive scan of kSelPer * kSelWarps counts (or pairs of 16-bit counts) in index order; returns the total.  All threads.
-__device__ __forceinline__ uint32_t scan_counts(uint32_t* cnt, uint32_t* warp_sum) {
-  static_assert(kSelPer * kSelWarps == kSelThreads, "a count a thread");
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  __syncthreads();
-  const uint32_t v = cnt[tid];
+// Exclusive scan over the threads (of counts, or of pairs of 16-bit counts); `total`: of all.  All threads.
+__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* warp_sum, uint32_t& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t incl = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += x;
   }
+  __syncthreads();                                 // (the scan before has been read)
   if (lane == 31) warp_sum[warp] = incl;
   __syncthreads();
-  uint32_t before = 0, total = 0;
+  uint32_t before = 0;
+  total = 0;
 #pragma unroll
   for (int w = 0; w < kSelWarps; ++w) {
     const uint32_t x = warp_sum[w];
     before += w < warp ? x : 0;
     total += x;
   }
-  cnt[tid] = before + incl - v;
-  __syncthreads();
-  return total;
+  return before + incl - v;
 }
 
 __global__ void __launch_bounds__(kSelThreads, 5) evict_select_kernel(const EvictParams p) {
@@ -81,7 +77,7 @@ __global__ void __launch_bounds__(kSelThreads, 5) evict_select_kernel(const Evic
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   __shared__ __align__(16) uint32_t key[kSelCap];  // ranks
   __shared__ __align__(16) uint32_t hist[2][kBins];
-  __shared__ uint32_t cnt[kSelPer * kSelWarps], warp_sum[kSelWarps];
+  __shared__ uint32_t warp_sum[kSelWarps];
   __shared__ uint32_t found[3];                    // bin, keys still to be taken from it, keys in it
   __shared__ uint32_t part[3][kSelWarps];
   __shared__ uint32_t peer[3][4][kMaxCluster];     // what the CTAs of the cluster have told this one, by occasion
@@ -90,7 +86,7 @@ __global__ void __launch_bounds__(kSelThreads, 5) evict_select_kernel(const Evic
   const int n = p.kv_len[r], m = p.keep[r], newest = p.tok_pos[r];
   const long long cap = (long long)p.max_pages_per_req * kPage;
   const bool over = n > 0 && n <= cap && m >= 0 && n > m;
-  // this CTA's keys: [lo, hi), kSelCap at a time; a place of theirs in a chunk is k * kSelThreads + thread
+  // this CTA's keys: [lo, hi), kSelCap at a time
   const int span = over ? ((n + cl - 1) / cl + 3) & ~3 : 0, lo = min(n, me * span), hi = min(n, lo + span);
   const size_t row = (size_t)line * cap;
   const long long first = (long long)newest - p.recent + 1;
@@ -137,7 +133,6 @@ __global__ void __launch_bounds__(kSelThreads, 5) evict_select_kernel(const Evic
   }
   if (cl > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");       // (this CTA is there: its shared memory may be written)
   const bool chunked = hi - lo > kSelCap;          // (longer than the shared memory of the cluster: chunks are read again in every pass)
-  auto used = [&](int base) { return min(kSelPer, (hi - base + kSelThreads - 1) / kSelThreads); };
   // every key of the CTA, with its index; a chunk other than the one in shared memory is loaded first
   int held = lo;
   auto fetch = [&](int base) {
@@ -188,11 +183,11 @@ __global__ void __launch_bounds__(kSelThreads, 5) evict_select_kernel(const Evic
       for (int base = lo; base < hi; base += kSelCap) {
         fetch(base);
         const int cnt_keys = min(hi - base, kSelCap);
+        const uint32_t most = bits == 0 ? 0u : 0xffffffffu >> (32 - bits);
 #pragma unroll 4
         for (int i = tid; i < cnt_keys; i += kSelThreads) {
-          const uint32_t x = key[i] - least;
-          // (below the range: wraps around to a large number)
-          if (key[i] != 0xffffffffu && (bits == 32 || x >> bits == 0)) atomicAdd(&h[x >> shift], 1u);
+          const uint32_t x = key[i] - least;       // (below the range: wraps around to a large number)
+          if (key[i] != 0xffffffffu && x <= most) atomicAdd(&h[x >> shift], 1u);
         }
       }
       if (cl > 1) cluster.sync();
@@ -256,11 +251,13 @@ __global__ void __launch_bounds__(kSelThreads, 5) evict_select_kernel(const Evic
     eq_first = __reduce_add_sync(0xffffffffu, lane < me ? peer[1][0][lane] : 0u);
   }
 
-  // Twice over the CTA's keys: the counts, of which the CTAs behind it are told, then the lists.  (One chunk, whose numbers are
-  // still in cnt the second time, unless the row is chunked.)
-  const uint32_t below = (1u << lane) - 1u;
+  // Twice over the CTA's keys: the counts, of which the CTAs behind it are told, then the lists.  A thread has neighbouring keys
+  // (an odd number of them, for the banks), so that its own counts and one scan number them in index order; the lists are put
+  // together where the ranks have been and leave in whole lines.
   const size_t half = (size_t)(cap / 2);
-  uint32_t bits = 0, frees = 0, moves = 0, eq_before = eq_first;       // frees, moves: of the chunks gone through; in the second go with those of the CTAs before
+  uint32_t frees = 0, moves = 0, eq_before = eq_first;       // of the chunks gone through; in the second go with those of the CTAs before
+  uint32_t at = 0, total = 0;                                // of this chunk, before this thread (freed places, keys to move in the high half)
+  unsigned long long pick = 0;                               // bit k: the thread's k-th key goes into a list
 #pragma unroll 1
   for (int go = 0; go < 2; ++go) {
     if (go == 1) {
@@ -278,56 +275,41 @@ __global__ void __launch_bounds__(kSelThreads, 5) evict_select_kernel(const Evic
     }
 #pragma unroll 1
     for (int base = lo; base < hi; base += kSelCap) {
-      const int in = hi - base, ks = used(base);
-      uint32_t total = 0;
+      const int in = min(hi - base, kSelCap), per = ((in + kSelThreads - 1) / kSelThreads) | 1;
+      static_assert(kSelCap / kSelThreads < 64, "a bit a key");
+      const int begin = min(in, tid * per), mine = min(in, begin + per) - begin;
       if (go == 0 || chunked) {
         fetch(base);
-        bits = 0;                                  // bit k: the thread's k-th key stays
+        uint32_t eq = 0, equal = 0;
         if (ties) {
-          cnt[tid] = 0;
-          __syncthreads();
-#pragma unroll 1
-          for (int k = 0; k < ks; ++k) {
-            const int i = k * kSelThreads + tid;
-            const uint32_t e = __ballot_sync(0xffffffffu, i < in && key[i] == least);
-            if (lane == 0) cnt[k * kSelWarps + warp] = __popc(e);
-          }
-          const uint32_t equal = scan_counts(cnt, warp_sum);
-#pragma unroll 1
-          for (int k = 0; k < ks; ++k) {
-            const int i = k * kSelThreads + tid;
-            const bool e = i < in && key[i] == least;
-            const uint32_t at = eq_before + cnt[k * kSelWarps + warp] + __popc(__ballot_sync(0xffffffffu, e) & below);
-            if (i < in && (key[i] > least || (e && at < need))) bits |= 1u << k;
-          }
+          for (int k = 0; k < mine; ++k) eq += key[begin + k] == least;
+          eq = eq_before + block_scan(eq, warp_sum, equal);
           eq_before += equal;
-          __syncthreads();                         // (cnt is read no more)
-        } else {
+        }
+        uint32_t c = 0;
+        pick = 0;
 #pragma unroll 4
-          for (int k = 0; k < ks; ++k)
-            if (k * kSelThreads + tid < in && key[k * kSelThreads + tid] >= least) bits |= 1u << k;
+        for (int k = 0; k < mine; ++k) {
+          const uint32_t x = key[begin + k];
+          const bool stays = ties ? x > least || (x == least && eq++ < need) : x >= least, under = base + begin + k < m;
+          c += under ? (stays ? 0u : 1u) : (stays ? 0x10000u : 0u);
+          pick |= (unsigned long long)(under != stays) << k;
         }
-        cnt[tid] = 0;
-        __syncthreads();
-#pragma unroll 2
-        for (int k = 0; k < ks; ++k) {             // places that become free (low half) and keys that move (high half)
-          const int i = k * kSelThreads + tid;
-          const bool s = bits >> k & 1;
-          const uint32_t f = __ballot_sync(0xffffffffu, i < in && base + i < m && !s), v = __ballot_sync(0xffffffffu, base + i >= m && s);
-          if (lane == 0) cnt[k * kSelWarps + warp] = __popc(f) | __popc(v) << 16;
-        }
-        total = scan_counts(cnt, warp_sum);
+        at = block_scan(c, warp_sum, total);
       }
       if (go == 1) {
-#pragma unroll 2
-        for (int k = 0; k < ks; ++k) {
-          const int i = k * kSelThreads + tid;
-          const bool s = bits >> k & 1, f = i < in && base + i < m && !s, v = base + i >= m && s;
-          const uint32_t bf = __ballot_sync(0xffffffffu, f), bv = __ballot_sync(0xffffffffu, v), c = cnt[k * kSelWarps + warp];
-          if (f) p.to[line * half + frees + (c & 0xffffu) + __popc(bf & below)] = base + i;
-          if (v) p.from[line * half + moves + (c >> 16) + __popc(bv & below)] = base + i;
+        const uint32_t n_free = total & 0xffffu, n_move = total >> 16;
+        __syncthreads();                           // (the ranks are read no more)
+        held = -1;
+        uint32_t f = at & 0xffffu, v = n_free + (at >> 16);
+        while (pick) {
+          const int i = base + begin + __ffsll((long long)pick) - 1;
+          pick &= pick - 1;
+          key[i < m ? f++ : v++] = i;
         }
-        __syncthreads();                           // (cnt is read no more)
+        __syncthreads();
+        for (int i = tid; i < n_free; i += kSelThreads) p.to[line * half + frees + i] = key[i];
+        for (int i = tid; i < n_move; i += kSelThreads) p.from[line * half + moves + i] = key[n_free + i];
       }
       frees += total & 0xffffu;
       moves += total >> 16;
