@@ -421,7 +421,9 @@ int fb_gate_commit(fb_ctx* ctx, const fb_pack* pk, const int32_t* slot_stats,
  * token, fb_token_attn attends to everything stored, fb_evict_kv cuts a cache
  * that has outgrown its bound.
  *
- * C = 64 * max_pages_per_req is the capacity of a request.  Per request:
+ * C = 64 * max_pages_per_req, at most 2^30, is the capacity of a request.  Calls on
+ * one cache, and calls with one workspace, are ordered by the caller (one stream, or
+ * events): two that overlap on the device race.  Per request:
  *   kv_len     [R_max] keys stored, the newest token's included.  0: none yet.
  *              Negative: no request in this row; no call reads or writes
  *              anything else of it.  Above C: FB_ST_BAD_STATE, row left as it is

@@ -372,16 +372,16 @@ int fb_gate_commit(fb_ctx* ctx, const fb_pack* pk, const int32_t* slot_stats, co
                          step_counters, status, (cudaStream_t)stream);
 }
 
-// What the calls that decode one token at a time have in common.  Capacities past 2^31 - 1 positions are refused:
-// lengths and positions are int32.
+// What the calls that decode one token at a time have in common.  Capacities past 2^30 keys are refused: lengths are int32,
+// and the kernels count a little beyond them.
 static int check_cache(fb_ctx* ctx, const fb_cache* kv, int fp8) {
   if (!kv) return fail(ctx, FB_ERR_INVALID_ARG, "cache is null");
   if (!kv->kv_len || !kv->page_table) return fail(ctx, FB_ERR_INVALID_ARG, "cache.kv_len or cache.page_table is null");
   if (fp8 >= 0 && fp8 != ctx->cfg.kv_fp8)
     return fail(ctx, FB_ERR_UNSUPPORTED, fp8 ? "8-bit KV pages need a context created with kv_fp8 = 1 (window_in_pages = 1, head_dim = 128)"
                                              : "this context holds 8-bit pages: use the call whose name ends in _fp8");
-  if ((long long)ctx->cfg.max_pages_per_req * fb::kPage > 0x7fffffffll)
-    return fail(ctx, FB_ERR_UNSUPPORTED, "max_pages_per_req * 64 must be below 2^31");
+  if ((long long)ctx->cfg.max_pages_per_req * fb::kPage > (1ll << 30))
+    return fail(ctx, FB_ERR_UNSUPPORTED, "max_pages_per_req * 64 must be at most 2^30");
   return FB_OK;
 }
 

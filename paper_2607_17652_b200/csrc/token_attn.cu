@@ -110,7 +110,7 @@ __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 
 // ---------------------------------------------------------------- the deal
 // Tiles of `len` stored keys (none where there is no request, nothing stored or the length is no length).
 __device__ __forceinline__ int tok_tiles(const TokenParams& p, int len, int tile) {
-  return len > 0 && len <= (long long)p.max_pages_per_req * kPage ? (len + tile - 1) / tile : 0;
+  return len > 0 && len <= (long long)p.max_pages_per_req * kPage ? (len - 1) / tile + 1 : 0;
 }
 __device__ __forceinline__ int tok_len(const TokenParams& p, int r) { return r < p.requests ? __ldcg(p.kv_len + r) : 0; }
 __device__ __forceinline__ long long tok_div(long long a, long long b) {        // (both below 2^31 but in absurd contexts)

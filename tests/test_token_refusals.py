@@ -60,7 +60,7 @@ def test_append_refuses():
     refused(ctx8, call8(ctx8, P, P, P, P, None, P, 0.0, P, None), B.FB_ERR_INVALID_ARG, b"null")
     assert lib.fb_append_kv(None, None, *ok) == B.FB_ERR_INVALID_ARG
     wide = B.Context(**dict(GOOD, max_pages_per_req=1 << 25))
-    refused(wide, call(wide, full(), *ok), B.FB_ERR_UNSUPPORTED, b"2^31")
+    refused(wide, call(wide, full(), *ok), B.FB_ERR_UNSUPPORTED, b"2^30")
 
 
 def cache_tensors(**over):
@@ -189,7 +189,7 @@ def test_evict_refuses():
     assert lib.fb_evict_kv(None, None, *ok) == B.FB_ERR_INVALID_ARG
     assert lib.fb_evict_workspace_bytes(None) == 0 and lib.fb_evict_workspace_bytes(ctx.handle) > 0
     wide = B.Context(**dict(GOOD, max_pages_per_req=1 << 25))
-    refused(wide, call(wide, full(), *ok), B.FB_ERR_UNSUPPORTED, b"2^31")
+    refused(wide, call(wide, full(), *ok), B.FB_ERR_UNSUPPORTED, b"2^30")
 
 
 def test_evict_refuses_tensors_that_do_not_fit(monkeypatch):
