@@ -50,7 +50,8 @@ struct TokenParams {
   int32_t* status;
   float* part_o;                         // [2 n_ctas][heads of a block][d] unnormalised outputs of the pieces
   float2* part_ml;                       // [2 n_ctas][heads of a block] reference (log2), sum
-  TokPieces* row_pieces;                 // [rows] (more than kDealAgain requests)
+  int2* cut;                             // [n_ctas] row that a CTA has begun and not finished, its pieces (0: none) (more than kDealAgain requests)
+  TokPieces* row_pieces;                 // [rows] (the same requests, weights only)
   float2* row_ml;                        // [rows][heads of a block] reference and sum of rows that were not cut (weights only)
   float* scores;                         // [requests][KV heads][capacity][group] (log2; weights only)
   int32_t requests, group, n_kv_heads, head_blocks, max_pages_per_req, num_pages, n_ctas, join_ctas;
@@ -163,8 +164,9 @@ __device__ __forceinline__ TokPieces tok_pieces(long long start, int nt, long lo
   k.n = (int)tok_div(start + nt - 1, share) - k.c0 + 1;
   return k;
 }
-// Up to as many requests the join finds the pieces from the lengths, while the stream still runs; for more the stream leaves
-// them per row, since a look at all lengths by every CTA of the join takes longer than one read more behind the stream.
+// Up to as many requests a CTA of the join has a row and finds its pieces from the lengths, while the stream still runs; for more the
+// stream leaves what it has cut per CTA: a CTA leaves one row at most, most rows are whole, and a look at all lengths by
+// every CTA of the join takes longer than one read more behind the stream.
 constexpr int kDealAgain = 32;
 
 // ---------------------------------------------------------------- the stream
@@ -463,6 +465,7 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
   pdl_wait_then_release();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rows = p.n_kv_heads * p.head_blocks;
+  if (tid == 0 && p.requests > kDealAgain) p.cut[blockIdx.x] = make_int2(0, 0);      // (the same thread sets it)
   int len = tok_len(p, lane);
   const TokDeal deal = tok_deal(p, S::kTile, len, 0);
   long long at = (long long)blockIdx.x * deal.share;
@@ -519,7 +522,9 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
     const int heads = min(HB, p.group - hb * HB);
     if (begins && tid == 0 && p.requests > kDealAgain) {
       const int rest = nt - seg;                 // of the row, to the CTAs behind this one
-      p.row_pieces[(size_t)r * rows + row] = TokPieces{(int)blockIdx.x, 1 + rest / sh_share + (rest % sh_share ? 1 : 0)};
+      const TokPieces k{(int)blockIdx.x, 1 + rest / sh_share + (rest % sh_share ? 1 : 0)};
+      if (W) p.row_pieces[(size_t)r * rows + row] = k;
+      if (rest) p.cut[blockIdx.x] = make_int2(r * rows + row, k.n);
     }
     for (int i = tid; i < heads * D; i += kTokThreads) {
       const int g = i / D, d = i % D;
@@ -685,35 +690,52 @@ __global__ void __launch_bounds__(kTokThreads) token_join_kernel(const TokenPara
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rows = p.n_kv_heads * p.head_blocks;
   const bool weights = W && (int)blockIdx.y >= p.join_ctas;
-  const int r = blockIdx.x / rows, row = blockIdx.x % rows, h = row / p.head_blocks, hb = row % p.head_blocks;
-  // (the kernel behind this one waits for this one alone: one CTA at least has to have waited for the stream)
-  const bool keeper = blockIdx.x == 0 && blockIdx.y == 0;
-  // (the lengths are older than the stream kernel, which waited itself before it let this one start)
-  const bool again = p.requests <= kDealAgain;
-  const int first = again ? tok_len(p, lane) : 0, len = tok_len(p, r), nt = tok_tiles(p, len, S::kTile);
-  const bool idle = nt == 0 || (weights && hb != 0);
-  if (!weights && nt == 0 && blockIdx.y == 0) {  // zeros where nothing is stored, a report where the length is no length
-    if (len > 0 && row == 0 && tid == 0) atomicOr(p.status, FB_ST_BAD_STATE);
-    if (len == 0) {
-      pdl_wait_only();                           // (before that the stream's predecessors may still read or write the output)
-      const int heads = min(HB, p.group - hb * HB);
-      uint4* o = reinterpret_cast<uint4*>(p.out + (((size_t)r * p.n_kv_heads + h) * p.group + hb * HB) * D);
-      for (int i = tid; i < heads * (D / 8); i += kTokThreads) o[i] = make_uint4(0, 0, 0, 0);
-    }
-  }
-  if (idle && !keeper) return;
+  // (the kernel behind this one waits for this one alone: one CTA at least has to have waited for the stream; the lengths are
+  // older than the stream kernel, which waited itself before it let this one start)
+  const bool keeper = blockIdx.x == 0 && blockIdx.y == 0, again = p.requests <= kDealAgain;
+  // zeros where nothing is stored, a report where the length is no length; the output only behind the wait, before which
+  // the stream's predecessors may still read or write it
+  auto empty_row = [&](int of, int n) {
+    if (n > (long long)p.max_pages_per_req * kPage && tid == 0) atomicOr(p.status, FB_ST_BAD_STATE);
+    if (n != 0) return;
+    pdl_wait_only();
+    uint4* o = reinterpret_cast<uint4*>(p.out) + (size_t)of * p.n_kv_heads * p.group * (D / 8);
+    for (int i = tid; i < p.n_kv_heads * p.group * (D / 8); i += kTokThreads) o[i] = make_uint4(0, 0, 0, 0);
+  };
+  int r = blockIdx.x / rows, row = blockIdx.x % rows, len = 0, nt = 0;
+  TokPieces k{0, 1};
   TokDeal deal{};
-  if (again && nt > 0) deal = tok_deal(p, S::kTile, first, r);
+  if (again || weights) {                        // CTA x has row x
+    if (r >= p.requests) return;                 // (the grid is wide enough for the CTAs of the deal too)
+    const int first = again ? tok_len(p, lane) : 0;
+    len = tok_len(p, r);
+    nt = tok_tiles(p, len, S::kTile);
+    if (!weights && blockIdx.y == 0 && row == 0) empty_row(r, len);
+    const bool idle = nt == 0 || (weights && row % p.head_blocks != 0);
+    if (idle && !keeper) return;
+    if (again && nt > 0) {
+      deal = tok_deal(p, S::kTile, first, r);
+      k = tok_pieces(deal.before + (long long)row * nt, nt, deal.share);
+    }
+    if (keeper || weights || k.n > 1) pdl_wait_only();
+    if (idle) return;
+  } else {                                       // CTA x has the row that CTA x of the stream has begun and not finished
+    if ((int)blockIdx.x >= p.n_ctas) return;
+    if (blockIdx.y == 0)
+      for (int of = blockIdx.x; of < p.requests; of += p.n_ctas) empty_row(of, tok_len(p, of));
+    pdl_wait_only();
+    const int2 cut = __ldcg(p.cut + blockIdx.x);
+    if (cut.y == 0) return;
+    k = TokPieces{(int)blockIdx.x, cut.y};
+    r = cut.x / rows;
+    row = cut.x % rows;
+  }
+  const int h = row / p.head_blocks, hb = row % p.head_blocks;
   auto pieces_of = [&](int of) {
     if (again) return tok_pieces(deal.before + (long long)of * nt, nt, deal.share);
     const int2 v = __ldcg(reinterpret_cast<const int2*>(p.row_pieces) + (size_t)r * rows + of);
     return TokPieces{v.x, v.y};
   };
-  TokPieces k{0, 1};
-  if (again && nt > 0) k = pieces_of(row);
-  if (keeper || weights || !again || k.n > 1) pdl_wait_only();
-  if (idle) return;
-  if (!again) k = pieces_of(row);
   if (!weights) {
     if (k.n == 1) return;
     for (int g = blockIdx.y; g < min(HB, p.group - hb * HB); g += p.join_ctas) {
@@ -797,7 +819,7 @@ __global__ void __launch_bounds__(kTokThreads) token_join_kernel(const TokenPara
 static int tok_heads(const fb_ctx* ctx) { return ctx->group > 8 ? 16 : 8; }
 static int tok_ctas(const fb_ctx* ctx) { return (ctx->group > 8 ? 2 : kTokCtasPerSm) * kSms; }
 
-struct TokWs { size_t part_ml, part_o, row_pieces, row_ml, scores, total; };
+struct TokWs { size_t part_ml, part_o, cut, row_pieces, row_ml, scores, total; };
 static TokWs tok_ws(const fb_ctx* ctx, bool weights) {
   const fb_config& c = ctx->cfg;
   const size_t hb = tok_heads(ctx), rows = (size_t)c.max_requests * c.n_kv_heads * ((ctx->group + hb - 1) / hb);
@@ -806,8 +828,9 @@ static TokWs tok_ws(const fb_ctx* ctx, bool weights) {
   TokWs w;
   w.part_ml = 0;
   w.part_o = w.part_ml + up(slots * hb * sizeof(float2));
-  w.row_pieces = w.part_o + up(slots * hb * c.head_dim * sizeof(float));
-  w.row_ml = w.row_pieces + (c.max_requests > kDealAgain ? up(rows * sizeof(TokPieces)) : 0);
+  w.cut = w.part_o + up(slots * hb * c.head_dim * sizeof(float));
+  w.row_pieces = w.cut + (c.max_requests > kDealAgain ? up(tok_ctas(ctx) * sizeof(int2)) : 0);
+  w.row_ml = w.row_pieces + (weights && c.max_requests > kDealAgain ? up(rows * sizeof(TokPieces)) : 0);
   w.scores = w.row_ml + (weights ? up(rows * hb * sizeof(float2)) : 0);
   w.total = w.scores + (weights ? up((size_t)c.max_requests * c.n_q_heads * c.max_pages_per_req * kPage * sizeof(float)) : 0);
   return w;
@@ -846,8 +869,9 @@ static int launch_token(fb_ctx* ctx, const TokenParams& p, cudaStream_t stream) 
   const long long pairs = (long long)c.max_requests * c.n_kv_heads, step = kWeightAt * kTokThreads;
   const long long blocks = ((long long)c.max_pages_per_req * kPage + step - 1) / step, want = 1 + 12 * kSms / pairs;
   const int slices = W ? (int)(want < blocks ? want : blocks) : 0;
-  // (a CTA a head where rows are few, one for all heads of a row where they fill the machine)
-  return cuda_err(ctx, launch_pdl(token_join_kernel<D, F8, NB, W>, dim3((unsigned)(pairs * p.head_blocks), p.join_ctas + slices), kTokThreads, 0, stream, p),
+  const long long rows = pairs * p.head_blocks, joins = c.max_requests <= kDealAgain ? rows : p.n_ctas;
+  const long long x = W && rows > joins ? rows : joins;
+  return cuda_err(ctx, launch_pdl(token_join_kernel<D, F8, NB, W>, dim3((unsigned)x, p.join_ctas + slices), kTokThreads, 0, stream, p),
                   "token_join_kernel launch");
 }
 template <int D, bool F8>
@@ -872,13 +896,15 @@ int launch_token_attn(fb_ctx* ctx, const fb_cache* kv, const void* q, const void
   p.k_scale = k_scale; p.v_scale = v_scale; p.out = static_cast<bf16*>(out); p.status = status;
   p.part_ml = reinterpret_cast<float2*>(base + w.part_ml);
   p.part_o = reinterpret_cast<float*>(base + w.part_o);
+  p.cut = reinterpret_cast<int2*>(base + w.cut);
   p.row_pieces = reinterpret_cast<TokPieces*>(base + w.row_pieces);
   p.row_ml = reinterpret_cast<float2*>(base + w.row_ml);
   p.scores = reinterpret_cast<float*>(base + w.scores);
   p.requests = c.max_requests; p.group = ctx->group; p.n_kv_heads = c.n_kv_heads;
   p.head_blocks = (ctx->group + hb - 1) / hb;
   p.max_pages_per_req = c.max_pages_per_req; p.num_pages = c.num_pages; p.n_ctas = tok_ctas(ctx);
-  const long long rows = (long long)c.max_requests * c.n_kv_heads * p.head_blocks, per_row = 8 * kSms / rows;
+  // (a CTA a head where rows that are cut are few, fewer where they may fill the machine)
+  const long long rows = (long long)c.max_requests * c.n_kv_heads * p.head_blocks, per_row = 8 * kSms / (rows < p.n_ctas ? rows : p.n_ctas);
   const int heads = ctx->group < hb ? ctx->group : hb;
   p.join_ctas = per_row < 1 ? 1 : per_row < heads ? (int)per_row : heads;
   p.sm_scale = ctx->sm_scale;
