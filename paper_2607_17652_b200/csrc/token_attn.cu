@@ -117,9 +117,11 @@ __device__ __forceinline__ int tok_len(const TokenParams& p, int r) { return r <
 __device__ __forceinline__ long long tok_div(long long a, long long b) {        // (both below 2^31 but in absurd contexts)
   return (a | b) >> 31 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
 }
-// Tiles of all rows (`total`) and of those of the requests before `upto`, and the share of a CTA: an equal one, but no
-// row in more than kMostPieces.  By a whole warp; `len`: the lane's length of the first 32 requests.
-constexpr int kMostPieces = 64;
+// Tiles of all rows (`total`) and of those of the requests before `upto`, and the share of a CTA: an equal one, but with few rows
+// at least sqrt(tiles of the longest / 32): a share takes its time tile by tile, the join 32 pieces at a time, and this is where
+// both together are least.  us, a row in at most 64 / 128 / 256 / 444 pieces (one request, 8 query heads on one KV head, GPU time):
+// 8,192 keys (128 tiles) 8.0 / 8.7 / 8.7 / 8.7, 32,768 13.3 / 11.8 / 13.8 / 13.9, 131,072 42.5 / 27.4 / 24.0 / 24.4.
+// By a whole warp; `len`: the lane's length of the first 32 requests.
 struct TokDeal { long long total, before, share; };
 __device__ __forceinline__ TokDeal tok_deal(const TokenParams& p, int tile, int len, int upto) {
   const int lane = threadIdx.x & 31, rows = p.n_kv_heads * p.head_blocks;
@@ -149,7 +151,7 @@ __device__ __forceinline__ TokDeal tok_deal(const TokenParams& p, int tile, int 
   TokDeal d;
   d.total = all * rows;
   d.before = before * rows;
-  d.share = max(max(tok_div(d.total + p.n_ctas - 1, p.n_ctas), (long long)((longest + kMostPieces - 1) / kMostPieces)), 1ll);
+  d.share = max(max(tok_div(d.total + p.n_ctas - 1, p.n_ctas), (long long)__float2int_rn(__fsqrt_rn(longest / 32.f))), 1ll);
   return d;
 }
 // The pieces of a row: of CTAs c0, c0 + 1, ...  The first lies in the odd slot of its CTA (the row starts in it), the others in the
@@ -683,7 +685,7 @@ template <int D, bool F8, int NB, bool W>
 __global__ void __launch_bounds__(kTokThreads) token_join_kernel(const TokenParams p) {
   using S = TokShape<D, F8>;
   constexpr int HB = 8 * NB, kLanes = D / 4, kGroups = kTokThreads / kLanes, kAhead = 8;
-  __shared__ float2 ml[kMostPieces + 2];
+  __shared__ float2 ml[kTokCtasPerSm * kSms];    // (a CTA leaves one piece of a row)
   __shared__ float4 red[kTokThreads];
   __shared__ float sums[kTokWarps], tops[kTokWarps];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

@@ -114,6 +114,21 @@ def test_long_and_ragged_batches(lens, heads, fp8):
     check_weights(case, weight, w)
 
 
+@pytest.mark.parametrize("heads,fp8", [((8, 1, 128), False), ((16, 1, 128), False), ((32, 1, 128), False), ((2, 1, 64), False),
+                                       ((8, 1, 128), True), ((16, 1, 128), True)])
+def test_one_long_row_in_many_pieces(heads, fp8):
+    """A single KV head: its keys are cut into hundreds of pieces, more than the join reads in a turn."""
+    case = Case([140001], heads, fp8, seed=140001)
+    ref, a, w = reference(case)
+    got, weight, status = attend(case, accumulate=True)
+    assert status == 0
+    check_out(case, got, ref, a)
+    check_weights(case, weight, w)
+    got, _, status = attend(case)
+    assert status == 0
+    check_out(case, got, ref, a)
+
+
 @pytest.mark.parametrize("heads,fp8", [((32, 8, 128), False), ((32, 8, 128), True), ((4, 1, 64), False), ((16, 1, 128), False),
                                        ((32, 32, 128), False), ((16, 1, 128), True)])
 @pytest.mark.parametrize("n", [1, 15, 16, 33, 95, 96, 97, 191, 193, 1000, 1536, 1537, 3001, 4031, 4096, 4097])
