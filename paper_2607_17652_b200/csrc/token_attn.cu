@@ -75,6 +75,8 @@ struct TokShape {
   static constexpr int kV = kRow / 128;                  // 16-byte loads of a V row by eight lanes
   static constexpr int kMb = D / 16;                     // row blocks of O^T
 };
+static_assert(TokShape<128, false>::kKeys * TokShape<128, false>::kRow == 32 * 128 && TokShape<64, false>::kKeys * TokShape<64, false>::kRow == 32 * 128,
+              "the keys of a step are a line a lane");
 static_assert(kPage % TokShape<128, false>::kKeys == 0 && kPage % TokShape<64, false>::kKeys == 0, "a step stays inside a page");
 
 __device__ __forceinline__ uint4 ld16(const char* p) {
@@ -424,6 +426,15 @@ __device__ __forceinline__ void tok_stream(const TokenParams& p, int r, int h, i
         }
     }
     if (work1) load_v(off1, rem - step);
+    if constexpr (NB > 1)
+      if (steps > 2 && rem > 2 * step && inside(page2)) {
+        // The step behind the next into L2, a line a lane: with 2 CTAs on an SM the loads of one step do not cover the latency of
+        // DRAM (32 heads on 2 of 128, 64 requests of 1,024 to 8,192 keys: 68.1 -> 66.8 us, 64 on 2 119 -> 115, 128 on 8, 16 requests of
+        // 16,384 to 32,768: 270 -> 255; a step further ahead is slower, and so is any with 3 CTAs: 184.5 -> 188.8).
+        const size_t off2 = page2 * page_bytes + in_head + lane * 128;
+        asm volatile("prefetch.global.L2 [%0];" :: "l"(p.k_pool + off2));
+        asm volatile("prefetch.global.L2 [%0];" :: "l"(p.v_pool + off2));
+      }
     work = work1;
     page1 = page2;
     rem -= step;
