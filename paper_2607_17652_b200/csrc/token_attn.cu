@@ -218,6 +218,15 @@ __device__ __forceinline__ void tok_stream(const TokenParams& p, int r, int h, i
   // (the stream starts before the queries are looked at)
   bool work = rem > 0 && inside(page0);
   if (work) { load_k(page0 * page_bytes + in_head, rem); load_v(page0 * page_bytes + in_head, rem); }
+  // The step behind it into L2, a line a lane, while the CTAs still start or change rows and DRAM has time: 64 requests of 1,024 to
+  // 8,192 keys, 32 heads on 8 of 128 183 -> 180 us, in 8 bits 103 -> 101, 64 on 4 117 -> 113; 128 of 100 to 600 42.0 -> 40.6; 256 of 64 to
+  // 256 45.5 -> 46.1.  (A second step 43 for the 128, 50 for the 256; in the kernel of few rows no gain.)
+  auto to_l2 = [&](size_t off) {
+    asm volatile("prefetch.global.L2 [%0];" :: "l"(p.k_pool + off + lane * 128));
+    asm volatile("prefetch.global.L2 [%0];" :: "l"(p.v_pool + off + lane * 128));
+  };
+  if constexpr (kStep > 0)
+    if (steps > 1 && rem > step && inside(page1)) to_l2(page1 * page_bytes + in_head);
   // queries: head c of each block, in the order in which the lanes hold a key's row
   uint32_t qf[NB][16 * S::kRow / 256 * (F8 ? 2 : 1)];
   float fac[NB][2];
@@ -426,15 +435,11 @@ __device__ __forceinline__ void tok_stream(const TokenParams& p, int r, int h, i
         }
     }
     if (work1) load_v(off1, rem - step);
+    // And all along with 2 CTAs on an SM, whose loads of one step do not cover the latency of DRAM: 32 heads on 2 of 128, 64 requests
+    // of 1,024 to 8,192 keys 68.1 -> 66.8 us, 64 on 2 119 -> 115, 128 on 8, 16 requests of 16,384 to 32,768 270 -> 255; a step further ahead
+    // is slower, and so is any with 3 CTAs: 184.5 -> 188.8.
     if constexpr (NB > 1)
-      if (steps > 2 && rem > 2 * step && inside(page2)) {
-        // The step behind the next into L2, a line a lane: with 2 CTAs on an SM the loads of one step do not cover the latency of
-        // DRAM (32 heads on 2 of 128, 64 requests of 1,024 to 8,192 keys: 68.1 -> 66.8 us, 64 on 2 119 -> 115, 128 on 8, 16 requests of
-        // 16,384 to 32,768: 270 -> 255; a step further ahead is slower, and so is any with 3 CTAs: 184.5 -> 188.8).
-        const size_t off2 = page2 * page_bytes + in_head + lane * 128;
-        asm volatile("prefetch.global.L2 [%0];" :: "l"(p.k_pool + off2));
-        asm volatile("prefetch.global.L2 [%0];" :: "l"(p.v_pool + off2));
-      }
+      if (steps > 2 && rem > 2 * step && inside(page2)) to_l2(page2 * page_bytes + in_head);
     work = work1;
     page1 = page2;
     rem -= step;
