@@ -544,6 +544,8 @@ __global__ void __launch_bounds__(kTokThreads, NB == 1 ? 3 : 2) token_attn_kerne
       if (W) p.row_pieces[(size_t)r * rows + row] = k;
       if (rest) p.cut[blockIdx.x] = make_int2(r * rows + row, k.n);
     }
+    // (four heads at once: 64 requests, 64 heads on 4 112.1 -> 110.1 us, 125 short ones, 16 on one 18.5 -> 17.9, the rest within 1 %)
+#pragma unroll 4
     for (int i = tid; i < heads * D; i += kTokThreads) {
       const int g = i / D, d = i % D;
       float m = sh_ml[0][g].x;
