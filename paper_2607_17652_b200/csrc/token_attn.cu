@@ -59,9 +59,9 @@ struct TokenParams {
 };
 
 // Caches of at most kFewCapacity keys in at most kFewRows (request, KV head) rows take a cluster each, where no weights are
-// asked for.  us, dealt / a cluster each (32 query and 8 KV heads of 128, GPU time): one request of 200 keys 6.8 / 5.3, of 700 7.4 /
-// 5.9, of 3,001 9.0 / 8.1, of 8,192 14.5 / 14.2; 4 requests of 500 to 3,000 keys 12.2 / 11.3, of 1,000 to 8,192 18.9 / 20.9; 16
-// requests of 500 to 2,000 20.5 / 21.8; with weights one request of 3,001 9.1 / 10.5.  And one launch less for the host.
+// asked for.  us, dealt / a cluster each (32 query and 8 KV heads of 128, GPU time): one request of 200 keys 5.4 / 5.1, of 700 6.9 /
+// 5.6, of 3,001 8.4 / 7.9, of 8,192 12.9 / 14.1; 4 requests of 500 to 3,000 keys 12.0 / 11.2, of 1,000 to 8,192 18.5 / 20.8; 16
+// requests of 500 to 2,000 19.2 / 21.3; with weights one request of 3,001 9.1 / 10.5.  And one launch less for the host.
 constexpr int kFewCapacity = 4096, kFewRows = 32;
 
 // How keys are laid out over lanes and steps, by the bytes of a row.
