@@ -99,7 +99,7 @@ _mt = None
 
 def lib() -> C.CDLL:
     """The loaded CUDA library.  Raises if it is missing (no fallback)."""
-    global _lib, _m, _mt
+    global _lib, _m
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(
@@ -154,17 +154,32 @@ def lib() -> C.CDLL:
                          "fb_evict_workspace_bytes"):
                 getattr(l, n).restype = I
         try:
-            from . import _marshal, _marshal_token
+            from . import _marshal
         except ImportError as e:
-            raise RuntimeError("the marshalling modules have not been built for this Python; run "
+            raise RuntimeError("the marshalling module has not been built for this Python; run "
                                "`python -m paper_2607_17652_b200.build`") from e
-        if _marshal_token.torch_version != torch.__version__.split("+")[0]:
-            raise RuntimeError("the marshalling module has been built for another torch; run "
-                               "`python -m paper_2607_17652_b200.build`")
-        _marshal_token.bind(*(C.cast(getattr(l, n), P).value for n in _TOKEN))
         _marshal.bind(*(C.cast(getattr(l, n), P).value for n in _FAST))
-        _lib, _m, _mt = l, _marshal, _marshal_token
+        _lib, _m = l, _marshal
     return _lib
+
+
+def _token():
+    """The marshalling module of the calls that decode one token at a time, loaded with the first of them: it is built
+    against one torch, and what goes through _marshal does not depend on that."""
+    global _mt
+    if _mt is None:
+        l = lib()
+        try:
+            from . import _marshal_token
+        except ImportError as e:
+            raise RuntimeError("the marshalling module of the token-by-token calls has not been built for this Python and "
+                               "torch; run `python -m paper_2607_17652_b200.build`") from e
+        if _marshal_token.torch_version != str(torch.__version__):
+            raise RuntimeError("the marshalling module of the token-by-token calls has been built for another torch "
+                               f"({_marshal_token.torch_version}); run `python -m paper_2607_17652_b200.build`")
+        _marshal_token.bind(*(C.cast(getattr(l, n), C.c_void_p).value for n in _TOKEN))
+        _mt = _marshal_token
+    return _mt
 
 
 class FlowBlockError(RuntimeError):
@@ -443,7 +458,7 @@ def fb_gate_commit(ctx: Context, pk: PackBuffers, slot_stats, st: DeviceState,
 def fb_append_kv(ctx: Context, cache: CacheState, k_new, v_new, k_pool, v_pool, status, rope_base: float = 0.0,
                  stream=None):
     """The newest token's K and V of every request to storage position kv_len - 1."""
-    rc = _mt.append(ctx._hv, ctx._sizes, _device(), cache, k_new, v_new, k_pool, v_pool, rope_base, status, _stream(stream))
+    rc = (_mt or _token()).append(ctx._hv, ctx._sizes, _device(), cache, k_new, v_new, k_pool, v_pool, rope_base, status, _stream(stream))
     if rc:
         ctx.check(rc)
 
@@ -451,7 +466,7 @@ def fb_append_kv(ctx: Context, cache: CacheState, k_new, v_new, k_pool, v_pool, 
 def fb_append_kv_fp8(ctx: Context, cache: CacheState, k_new, v_new, k_pool8, v_pool8, k_scale, v_scale, status,
                      rope_base: float = 0.0, stream=None):
     """The same into 8-bit (E4M3) pages."""
-    rc = _mt.append_fp8(ctx._hv, ctx._sizes, _device(), cache, k_new, v_new, k_pool8, v_pool8, rope_base, status,
+    rc = (_mt or _token()).append_fp8(ctx._hv, ctx._sizes, _device(), cache, k_new, v_new, k_pool8, v_pool8, rope_base, status,
                        _stream(stream), k_scale, v_scale)
     if rc:
         ctx.check(rc)
@@ -460,7 +475,7 @@ def fb_append_kv_fp8(ctx: Context, cache: CacheState, k_new, v_new, k_pool8, v_p
 def fb_token_attn(ctx: Context, cache: CacheState, q, k_pool, v_pool, out, ws, status, accumulate: bool = False,
                   stream=None):
     """One query token per request over all it has stored; ``accumulate``: its softmax weights are added to kv_weight."""
-    rc = _mt.token_attn(ctx._hv, ctx._sizes, _device(), cache, q, k_pool, v_pool, out, accumulate, ws, status, _stream(stream))
+    rc = (_mt or _token()).token_attn(ctx._hv, ctx._sizes, _device(), cache, q, k_pool, v_pool, out, accumulate, ws, status, _stream(stream))
     if rc:
         ctx.check(rc)
 
@@ -468,7 +483,7 @@ def fb_token_attn(ctx: Context, cache: CacheState, q, k_pool, v_pool, out, ws, s
 def fb_token_attn_fp8(ctx: Context, cache: CacheState, q, k_pool8, v_pool8, k_scale, v_scale, out, ws, status,
                       accumulate: bool = False, stream=None):
     """The same over 8-bit (E4M3) pages."""
-    rc = _mt.token_attn_fp8(ctx._hv, ctx._sizes, _device(), cache, q, k_pool8, v_pool8, out, accumulate, ws, status,
+    rc = (_mt or _token()).token_attn_fp8(ctx._hv, ctx._sizes, _device(), cache, q, k_pool8, v_pool8, out, accumulate, ws, status,
                            _stream(stream), k_scale, v_scale)
     if rc:
         ctx.check(rc)
@@ -477,7 +492,7 @@ def fb_token_attn_fp8(ctx: Context, cache: CacheState, q, k_pool8, v_pool8, k_sc
 def fb_evict_kv(ctx: Context, cache: CacheState, keep, recent: int, sinks: int, k_pool, v_pool, ws, status, stream=None):
     """Cuts every cache of more than keep[r] keys to that many: the last ``recent`` and the first ``sinks`` positions,
     then those of greatest accumulated weight.  bf16 or 8-bit pools, as the context says."""
-    rc = _mt.evict(ctx._hv, ctx._sizes, _device(), cache, keep, recent, sinks, k_pool, v_pool, ws, status, _stream(stream))
+    rc = (_mt or _token()).evict(ctx._hv, ctx._sizes, _device(), cache, keep, recent, sinks, k_pool, v_pool, ws, status, _stream(stream))
     if rc:
         ctx.check(rc)
 

@@ -7,9 +7,10 @@ without a GPU.  Objects are rebuilt only when a source or header is newer.
 """
 from __future__ import annotations
 
-import importlib.metadata
 import importlib.util
 import os
+import runpy
+import shutil
 import subprocess
 import sys
 import sysconfig
@@ -40,17 +41,30 @@ def _deps():
     return hs
 
 
+def torch_version(torch_dir: str) -> str:
+    """``torch.__version__`` of the torch installed there, without importing it."""
+    return runpy.run_path(os.path.join(torch_dir, "version.py"))["__version__"]
+
+
 def _build_marshal_token(run, force: bool, hdr_time: float) -> None:
-    """Rebuilt for another torch too: it looks into torch's own structures."""
+    """Rebuilt for another torch too: it looks into torch's own structures.  Only the token-by-token calls go through it,
+    so that where torch, its headers or a C++ compiler are missing it is left out, and those calls say so."""
     src, stamp = os.path.join(CSRC, "marshal_token.cpp"), os.path.join(HERE, "build", "marshal_token.torch")
-    version = importlib.metadata.version("torch")
+    spec, cxx = importlib.util.find_spec("torch"), os.environ.get("CXX", "g++")
+    torch_dir = spec.submodule_search_locations[0] if spec else ""
+    inc, lib = os.path.join(torch_dir, "include"), os.path.join(torch_dir, "lib")
+    missing = ("torch is missing" if not spec else
+               "torch's headers are missing" if not os.path.exists(os.path.join(inc, "torch", "csrc", "autograd", "python_variable.h")) else
+               f"the C++ compiler {cxx} is missing" if not shutil.which(cxx) else "")
+    if missing:
+        sys.stderr.write(f"{missing}: built without fb_append_kv, fb_token_attn and fb_evict_kv for Python\n")
+        return
+    version = torch_version(torch_dir)
     same = os.path.exists(stamp) and open(stamp).read() == version
     if not force and same and os.path.exists(MARSHAL_TOKEN) and \
-            os.path.getmtime(MARSHAL_TOKEN) >= max(os.path.getmtime(src), hdr_time):
+            os.path.getmtime(MARSHAL_TOKEN) >= max(os.path.getmtime(src), os.path.getmtime(__file__), hdr_time):
         return
-    torch_dir = importlib.util.find_spec("torch").submodule_search_locations[0]
-    inc, lib = os.path.join(torch_dir, "include"), os.path.join(torch_dir, "lib")
-    run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall",
+    run([cxx, "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", f'-DFB_TORCH_VERSION="{version}"',
          "-I", sysconfig.get_paths()["include"], "-I", inc, "-I", os.path.join(inc, "torch", "csrc", "api", "include"),
          "-L", lib, src, "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", MARSHAL_TOKEN])
     with open(stamp, "w") as f:
@@ -91,10 +105,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
             os.path.getmtime(MARSHAL) < max(os.path.getmtime(src), hdr_time):
         run([os.environ.get("CC", "gcc"), "-O2", "-shared", "-fPIC", "-Wall",
              "-I", sysconfig.get_paths()["include"], src, "-o", MARSHAL])
-    _build_marshal_token(run, force, hdr_time)
     if logs:
         with open(os.path.join(HERE, "build", "ptxas.log"), "w") as f:
             f.write("\n".join(logs))
+    _build_marshal_token(run, force, hdr_time)      # (last: nothing else waits for it)
     return LIB
 
 

@@ -2,12 +2,12 @@
 // number of elements, the contiguity and the device that the call needs before its pointer is taken.  Asking a tensor for
 // these through its Python methods takes 0.3 us each, 3 to 4 us a call of a step that runs for 2 to 8 us on the GPU, so this module
 // is built against torch's headers and looks into the tensor itself (a call's marshalling 4.1 -> 0.4 us).  The entry points
-// come by address (bind), as there.
+// come by address (bind), as there.  FB_TORCH_VERSION: torch.__version__ of those headers, whole, since the version in the headers
+// leaves out what tells one pre-release from the next.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
 #include <torch/csrc/autograd/python_variable.h>
-#include <torch/version.h>
 
 #include "../../include/flowblock.h"
 
@@ -212,6 +212,6 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal_token", "argument marshal
 PyMODINIT_FUNC PyInit__marshal_token(void) {
   for (int i = 0; i < 5; ++i) if (!(s_cache[i] = PyUnicode_InternFromString(k_cache[i]))) return nullptr;
   PyObject* m = PyModule_Create(&module);
-  if (m && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) < 0) { Py_DECREF(m); return nullptr; }
+  if (m && PyModule_AddStringConstant(m, "torch_version", FB_TORCH_VERSION) < 0) { Py_DECREF(m); return nullptr; }
   return m;
 }
