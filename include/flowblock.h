@@ -493,8 +493,8 @@ int fb_token_attn_fp8(fb_ctx* ctx, const fb_cache* cache, const void* q,
 
 /* Cuts every cache that holds more than keep[r] keys to keep[r] of them, for each
  * KV head by itself.  The keys that stay are the first keep[r] in this order:
- * protected ones (kv_pos < sinks, or among the last `recent` positions, kv_pos >
- * tok_pos - recent) by storage position, then the others by greater kv_weight and
+ * protected ones (kv_pos < sinks, or kv_pos > tok_pos - recent: the last `recent`
+ * positions, and any above tok_pos, with recent = 0 too) by storage position, then the others by greater kv_weight and
  * then by lower storage position; a NaN weight ranks below every number.  With m = keep[r]: the
  * i-th storage position below m that becomes free takes over what the i-th
  * position at or above m that stays holds, K and V rows, kv_pos and kv_weight;

@@ -1,5 +1,5 @@
 // fb_evict_kv: cuts every cache that holds more than keep[r] keys to that many, per KV head: protected keys first (the
-// first `sinks` and the last `recent` positions), then by accumulated attention weight, the lower index on ties.
+// first `sinks` and the last `recent` positions, and any above tok_pos), then by accumulated attention weight, the lower index on ties.
 //
 // Attention does not see in which order keys are stored (they are stored rotated), so nothing moves but what has to:
 // with m = keep[r], the keys that stay at or above m take the places below m that become free, i-th to i-th.  Sources
@@ -38,8 +38,8 @@ struct EvictParams {
   int32_t n_kv_heads, max_pages_per_req, num_pages, recent, sinks;
 };
 
-// Rank of a key as an unsigned number: protected keys above all, a NaN below all, -0 as 0.  `first`: the first of the last
-// `recent` positions.
+// Rank of a key as an unsigned number: protected keys above all, a NaN below all, -0 as 0.  `first`: the first position above
+// tok_pos - recent, where there is any that 32 bits hold.
 struct Guarded { int sinks, first; bool any; };
 __device__ __forceinline__ uint32_t rank_of(float w, int pos, const Guarded& g) {
   const uint32_t u = __float_as_uint(w + 0.f);
@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(kSelThreads, 5) evict_select_kernel(const Evic
   const int span = over ? ((n + cl - 1) / cl + 3) & ~3 : 0, lo = min(n, me * span), hi = min(n, lo + span);
   const size_t row = (size_t)line * cap;
   const long long first = (long long)newest - p.recent + 1;
-  const Guarded guard{p.sinks, (int)max(first, -0x80000000ll), p.recent > 0};
+  const Guarded guard{p.sinks, (int)min(max(first, -0x80000000ll), 0x7fffffffll), first <= 0x7fffffffll};
   // A chunk's ranks from its weights and positions, four at a time (a row starts on 256 bytes and is whole pages long, so that
   // the last four stay inside it).
   uint32_t low = 0xffffffffu, high = 0, guards = 0; // of the unprotected ranks, and protected keys
