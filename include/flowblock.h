@@ -425,8 +425,10 @@ int fb_gate_commit(fb_ctx* ctx, const fb_pack* pk, const int32_t* slot_stats,
  * one cache, and calls with one workspace, are ordered by the caller (one stream, or
  * events): two that overlap on the device race.  Per request:
  *   kv_len     [R_max] keys stored, the newest token's included.  0: none yet.
- *              Negative: no request in this row; no call reads or writes
- *              anything else of it.  Above C: FB_ST_BAD_STATE, row left as it is
+ *              Negative: no request in this row; nothing of it is written and
+ *              nothing that it holds changes a result (all arrays have R_max
+ *              rows: a call may load any of them before it looks at kv_len).
+ *              Above C: FB_ST_BAD_STATE, row left as it is
  *   tok_pos    [R_max] absolute position of the newest token (what its key is
  *              rotated by; equal to kv_len - 1 until something is evicted)
  *   kv_pos     [R_max, n_kv_heads, C] absolute position of every stored key
@@ -436,7 +438,9 @@ int fb_gate_commit(fb_ctx* ctx, const fb_pack* pk, const int32_t* slot_stats,
  * kv_pos and kv_weight are what fb_evict_kv goes by; a caller that never evicts
  * may leave both NULL (each KV head has its own because heads evict different
  * keys).  kv_len may be the prefix_len of an fb_state, page_table its
- * page_table.  The caller advances kv_len and tok_pos. */
+ * page_table.  The caller advances kv_len and tok_pos.  Requests may share pages
+ * that are only read; a page that a call writes (the newest token's, any of a
+ * cache that is cut) stands once in the tables of all live requests. */
 typedef struct {
   int32_t* kv_len;
   int32_t* tok_pos;
@@ -480,7 +484,9 @@ int fb_append_kv_fp8(fb_ctx* ctx, const fb_cache* cache, const void* k_new,
  * fp32 scores, statistics and sums; the softmax weights are rounded to the 16-bit
  * type of the second product (bf16; fp16 where the pages hold 8 bits), the
  * output to bf16.  8-bit pages: K and V are taken as byte * scale exactly, the
- * queries as fp16 after an exact power-of-two scaling per row. */
+ * queries as fp16 after an exact power-of-two scaling per row (exact but for
+ * elements more than 2^32 below the largest of their row, which are off by at
+ * most 2^-40 of that largest one). */
 size_t fb_token_workspace_bytes(const fb_ctx* ctx, int32_t accumulate);
 int fb_token_attn(fb_ctx* ctx, const fb_cache* cache, const void* q,
                   const void* k_pool, const void* v_pool, void* out,
@@ -494,17 +500,18 @@ int fb_token_attn_fp8(fb_ctx* ctx, const fb_cache* cache, const void* q,
 /* Cuts every cache that holds more than keep[r] keys to keep[r] of them, for each
  * KV head by itself.  The keys that stay are the first keep[r] in this order:
  * protected ones (kv_pos < sinks, or kv_pos > tok_pos - recent: the last `recent`
- * positions, and any above tok_pos, with recent = 0 too) by storage position, then the others by greater kv_weight and
- * then by lower storage position; a NaN weight ranks below every number.  With m = keep[r]: the
- * i-th storage position below m that becomes free takes over what the i-th
- * position at or above m that stays holds, K and V rows, kv_pos and kv_weight;
- * nothing else moves, and kv_len becomes m.  (Attention does not see the order in
+ * positions, and any above tok_pos, with recent = 0 too) by storage position,
+ * then the others by greater kv_weight and then by lower storage position; a NaN
+ * weight ranks below every number.  With m = keep[r]: the i-th storage position
+ * below m that becomes free takes over what the i-th position at or above m that
+ * stays holds, K and V rows, kv_pos and kv_weight; nothing else moves, and kv_len
+ * becomes m.  (Attention does not see the order in
  * which keys are stored.)  Requests with keep[r] < 0 or kv_len <= keep[r] stay as
  * they are; pages behind the new kv_len are the caller's again.
  *   keep          [R_max] int32, DEVICE pointer
  *   recent, sinks at least 0
  *   k_pool,v_pool the pools of the context, bf16 or 8-bit (rows are moved as they
- *                 are); pages that requests share must not be evicted from
+ *                 are)
  *   ws            fb_evict_workspace_bytes(ctx) bytes of device scratch, 256-byte
  *                 aligned; nothing in it outlives the call
  * A request with a page outside the pool below kv_len is left as it is and
