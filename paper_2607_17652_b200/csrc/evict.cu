@@ -7,13 +7,13 @@
 //
 // Kernel 1, a cluster of 1 to 8 CTAs per (request, KV head): the rank of the last key that stays, by counting.  The range
 // of the ranks is cut into 512 bins, the bin that holds the boundary into 512 again, until all keys of a bin stay
-// (two or three times, 512 bins that follow the range spread the counts over many addresses); then the lists of freed
+// (two or three times as a rule, four at most; 512 bins that follow the range spread the counts over many addresses); then the lists of freed
 // places and of keys to move, both in index order by the threads' own counts and one scan.  Bound by its chain of block-wide steps: loops
 // are kept short, since every CTA runs the code once, and what goes between the CTAs of a cluster is kept small (one request
 // of 28,123 keys: digits of 11 bits and code unrolled over keys in registers 28 us, this form 16).  Reads 8 bytes a stored key.
 // Kernel 2: the rows of K and V, the weights and the positions, eight rows a warp under way.
 // HBM-bound where many move, by rows of 128 to 256 bytes that lie apart: 64 requests cut from 1,024 to 8,192 keys to 2,000 move
-// 0.46 GB in bf16 at 4.4 TB/s, 0.23 GB in 8 bits at 3.7 TB/s; neither more rows under way nor more warps change that.
+// 0.49 GB in bf16 in 93 us (5.3 TB/s), 0.25 GB in 8 bits in 53 us (4.6 TB/s); neither more rows under way nor more warps change that.
 #include <cooperative_groups.h>
 
 #include "fb_common.cuh"
@@ -395,7 +395,9 @@ int launch_evict(fb_ctx* ctx, const fb_cache* kv, const int32_t* keep, int recen
   p.n_kv_heads = c.n_kv_heads; p.max_pages_per_req = c.max_pages_per_req; p.num_pages = c.num_pages;
   p.recent = recent; p.sinks = sinks;
   const long long rows = (long long)c.max_requests * c.n_kv_heads, cap = (long long)c.max_pages_per_req * kPage;
-  // CTAs of a row: enough that its keys stay in registers, and more where rows are few (each has less to go through)
+  // CTAs of a row: enough for its keys in shared memory, and more where rows are few (each has less to go through).  Both by the
+  // capacity and the rows of the context, since the lengths are only known on the device: 64 caches of 2,112 keys take 17 us in
+  // a context for 2,112 keys, 39 in one for 32,768, and one of 28,123 takes 20 alone in its context, 37 as the only one of 64 rows.
   int cl = 1;
   while (cl < 8 && cl * (long long)kSelCap < cap) cl *= 2;
   while (cl < 8 && rows * cl * 2 <= kSms && cl * 512ll < cap) cl *= 2;

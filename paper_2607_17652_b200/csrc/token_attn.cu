@@ -19,8 +19,8 @@
 // the A fragments of two k-steps, and of the rows 2t, 2t+1, 2t+8, 2t+9 of V the 16 bytes that its eight (row block, row)
 // places need; pairs of V rows are interleaved by byte permutes, P^T is S^T's fragment transposed by movmatrix.  No
 // shared memory, no barrier, no address arithmetic but one base per step, and the next step's K and V are in flight
-// while this one's products run.  The tensor pipe (legacy mma.sync) is far from its rate: 4 d x 16 products a key
-// against 256 bytes from memory.
+// while this one's products run.  The tensor pipe (legacy mma.sync) is far from its rate: 16 d multiply-adds a key for a
+// block of 8 heads against 4 d bytes from memory (2 d in 8 bits).
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -61,7 +61,9 @@ struct TokenParams {
 // Caches of at most kFewCapacity keys in at most kFewRows (request, KV head) rows take a cluster each, where no weights are
 // asked for.  us, dealt / a cluster each (32 query and 8 KV heads of 128, GPU time): one request of 200 keys 5.4 / 5.1, of 700 6.9 /
 // 5.6, of 3,001 8.4 / 7.9, of 8,192 12.9 / 14.1; 4 requests of 500 to 3,000 keys 12.0 / 11.2, of 1,000 to 8,192 18.5 / 20.8; 16
-// requests of 500 to 2,000 19.2 / 21.3; with weights one request of 3,001 9.1 / 10.5.  And one launch less for the host.
+// requests of 500 to 2,000 19.2 / 21.3; with weights one request of 3,001 9.1 / 10.5.  And one launch less for the host.  These in
+// contexts whose capacity is the longest length; the capacity is all that the host knows, and room above the lengths costs:
+// one request of 200, 700 and 3,001 keys takes 6.4, 6.6 and 8.0 where the capacity is 4,096, 5.4, 6.6 and 8.4 (dealt) where it is 32,768.
 constexpr int kFewCapacity = 4096, kFewRows = 32;
 
 // How keys are laid out over lanes and steps, by the bytes of a row.
@@ -246,7 +248,8 @@ __device__ __forceinline__ void tok_stream(const TokenParams& p, int r, int h, i
       }
       float inv = 1.f;
       if constexpr (F8) {
-        // fp16 after an exact scaling of the row by a power of two: its largest element comes to [2^15, 2^16)
+        // fp16 after an exact scaling of the row by a power of two: its largest element comes to [2^15, 2^16), so that the
+        // elements down to 2^-32 of it are exact (fp16 ends at 2^-24, a bf16 has 8 bits) and no other is off by more than 2^-40 of it
         float top = 0.f;
 #pragma unroll
         for (int u = 0; u < kQ; ++u)
@@ -388,6 +391,9 @@ __device__ __forceinline__ void tok_stream(const TokenParams& p, int r, int h, i
             for (int i = 0; i < S::kMb; ++i) { o[nb][i][j] *= f; o[nb][i][j + 2] *= f; }
           }
       }
+      // The weights are rounded to the 16 bits that the second product takes, by at most 2^-8 of themselves in bf16 (2^-11 in fp16):
+      // outputs are 2.3e-3 from 64 bits in the 2-norm, 1.7e-3 were they rounded once at the end, as in the block attention.  Their
+      // remainders as a second operand would double the instructions and the registers of this product.
       uint32_t pt[NB][S::kSub][2];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
@@ -955,6 +961,8 @@ static int launch_token(fb_ctx* ctx, const TokenParams& p, cudaStream_t stream) 
   }
   if (int e = cuda_err(ctx, launch_pdl(token_attn_kernel<D, F8, NB, W>, p.n_ctas, kTokThreads, 0, stream, p), "token_attn_kernel launch"))
     return e;
+  // (slices by the rows of the context, since what they hold is only known on the device: one request of 28,123 keys with weights takes
+  // 24.5 us alone in its context, 33.3 as the only one of 64 rows)
   const long long pairs = (long long)c.max_requests * c.n_kv_heads, step = kWeightAt * kTokThreads;
   const long long blocks = ((long long)c.max_pages_per_req * kPage + step - 1) / step, want = 1 + 12 * kSms / pairs;
   const int slices = W ? (int)(want < blocks ? want : blocks) : 0;
