@@ -440,7 +440,8 @@ int fb_gate_commit(fb_ctx* ctx, const fb_pack* pk, const int32_t* slot_stats,
  * keys).  kv_len may be the prefix_len of an fb_state, page_table its
  * page_table.  The caller advances kv_len and tok_pos.  Requests may share pages
  * that are only read; a page that a call writes (the newest token's, any of a
- * cache that is cut) stands once in the tables of all live requests. */
+ * cache that is cut) stands once among the entries that hold keys of all
+ * requests (entries behind kv_len may be anything). */
 typedef struct {
   int32_t* kv_len;
   int32_t* tok_pos;
